@@ -28,7 +28,8 @@
  *
  * Around that path: intattn_quantize (Sec. 2.1, Eq. quant, scales left in device memory),
  * intattn_forward_dynamic (the forward on such device-resident scales) and
- * intattn_index_softmax (Sec. 3.1-3.2 alone, on INT32 logits).
+ * intattn_index_softmax (Sec. 3.1-3.2 alone, on INT32 logits).  For serving from a paged INT8 cache: intattn_rope,
+ * intattn_cache_append, intattn_cache_forward and intattn_cache_evict.
  *
  * The L x L score matrix never reaches HBM.  Results are a deterministic integer
  * function of the inputs (no dependence on tiling or launch shape).
@@ -240,6 +241,151 @@ typedef struct {
 
 /* Enqueues the operator on hip_stream and returns without waiting.  Allocates nothing. */
 INTATTN_API int intattn_index_softmax(intattn_ctx *ctx, const intattn_softmax_args *args, void *hip_stream);
+
+/*
+ * Operators around a paged INT8 key/value cache: rotary positions on Q and K, new tokens into the cache, attention of
+ * the newest tokens over it, and eviction.  A cache is a pool of pages of page_size keys each; row b of the table names
+ * the pages of sequence b in order, so that its key number j (its slot) is key j % page_size of page table[b][j / page_size].
+ * An entry that is not in 0 .. n_pages - 1 stands for a page that is not there: its keys are hidden, and nothing is written
+ * to them.  lens[b], the number of slots in use, is taken as at least 0 and at most max_pages * page_size; the caller
+ * keeps it.  Sequences may share pages that none of them writes to.  Scales that are not finite and > 0 cannot be
+ * reported by return code: rows that they belong to come out as zeros.  Everything in the struct but the scalars is
+ * DEVICE memory that the kernels read when they run: a captured call sees the lengths, tables and scales of its replay.
+ */
+typedef struct {
+    int32_t B, Hkv, d;         /* sequences, 1 .. 65535; KV heads, 1 .. 65535; head dimension, 64 or 128   */
+    int32_t n_pages, page_size; /* pages in the pool, >= 1; keys of a page, 1 .. 65536 (multiples of 16 run fastest) */
+    int32_t max_pages;         /* table entries of a sequence, >= 1; max_pages * page_size <= 2^30          */
+    int32_t scale_mode;        /* 0: one float per scale array; 1: one per KV head                          */
+    int32_t reserved;          /* must be 0                                                                 */
+    int8_t *k, *v;             /* [n_pages, Hkv, page_size, d], d contiguous, 16-byte aligned               */
+    int64_t k_stride[3], v_stride[3]; /* BYTES between pages, heads and keys, multiples of 16, key stride >= d */
+    const int32_t *table;      /* [B, max_pages]                                                            */
+    int64_t table_stride;      /* ELEMENTS between the rows of the table, >= max_pages (B > 1)              */
+    const int32_t *lens;       /* [B]                                                                       */
+    const float *scale_k, *scale_v;
+} intattn_cache;
+
+/* Rotary positions with up to four axes (time, height, width, ...).  Pair i of a row's first `rot` channels, (a, b),
+ * becomes (a cos t - b sin t, a sin t + b cos t) with t = pos[axis[i]] * freq[i]; the channels behind stay.  The angle is
+ * the product in 64 bits and the rotation is evaluated in 64 bits and rounded once to 32.  inverse: t = -pos * freq,
+ * which is the gradient of the rotation (its transpose).  */
+typedef struct {
+    int32_t rot;               /* rotated channels, a multiple of 16, at most d and 256                     */
+    int32_t pairing;           /* pair i is 0: channels 2 i and 2 i + 1; 1: channels i and i + rot / 2      */
+    int32_t n_axes;            /* 1 .. 4                                                                    */
+    int32_t inverse;           /* 0 or 1                                                                    */
+    const int32_t *pos;        /* DEVICE [n_axes, B, L], any sign                                           */
+    int64_t pos_stride[3];     /* ELEMENTS between axes, sequences and tokens, >= 0                         */
+    const double *freq;        /* DEVICE [rot / 2]: radians per position                                    */
+    uint8_t axis[128];         /* axis of each of the rot / 2 pairs                                         */
+} intattn_rotary;
+
+/* Rotary positions on one or two tensors [B, H[i], L, d] with the same positions (Q and K of a layer).  dst may be
+ * src with the same strides, else the tensors must not overlap.  src, dst and their BYTE strides (B, H, L) are
+ * multiples of 16, the L strides of src at least a row; d is a multiple of 16, at most 1024. */
+typedef struct {
+    int32_t B, L, d;
+    int32_t dtype;             /* 0 = fp32, 1 = fp16, 2 = bf16 */
+    int32_t H[2];              /* H[0] >= 1; H[1] = 0: one tensor */
+    const void *src[2];
+    void *dst[2];
+    int64_t src_stride[2][3], dst_stride[2][3];
+    intattn_rotary rotary;
+} intattn_rope_args;
+
+/* Enqueues the rotation on hip_stream.  Allocates nothing. */
+INTATTN_API int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *args, void *hip_stream);
+
+/*
+ * New tokens: K rotated (rotary.rot = 0: not), K and V quantized with the cache's scales (Sec. 2.1, Eq. quant: the nearest
+ * integer of the fp32 quotient x / s, ties to even, clamped to +-127) and written to slots lens[b] - n_new[b] + t, so the lengths
+ * already count the new tokens; Q, where Hq > 0, rotated and quantized with a scale for each token and head,
+ * s = max|q| / 127 (max|q| floored at 1e-12), as intattn_cache_forward takes it.  Sequence b has n_new[b] tokens, the rest
+ * of its L are padding: nothing is written for their K and V, their integers and scales of Q are 0.  Inputs must be finite.
+ */
+typedef struct {
+    int32_t L, Hq;             /* tokens of a sequence, 1 .. 131071; query heads, a multiple of Hkv, or 0    */
+    int32_t dtype;             /* of q, k, v: 0 = fp32, 1 = fp16, 2 = bf16                                   */
+    int32_t reserved;          /* must be 0                                                                  */
+    const void *q, *k, *v;     /* [B, H, L, d], BYTE strides of B, H, L, all multiples of 16; q NULL if Hq = 0 */
+    int64_t q_stride[3], k_stride[3], v_stride[3];
+    const int32_t *n_new;      /* [B], taken as 0 .. min(L, lens[b]); NULL: min(L, lens[b])                  */
+    int8_t *q_out;             /* [B, Hq, L, d], BYTE strides multiples of 16                                */
+    int64_t q_out_stride[3];
+    float *q_scale;            /* [B, Hq, L] contiguous                                                      */
+    intattn_rotary rotary;     /* inverse must be 0                                                          */
+    float *weight;             /* optional [B, Hkv, slots]: 0 is written for each new key                    */
+    int32_t *order;            /* optional [B, Hkv, slots]: first[b] + t is written for each new key (first  */
+    const int32_t *first;      /* NULL: its slot); [B], number of the first new token of the sequence         */
+    int64_t weight_stride[2], order_stride[2]; /* ELEMENTS between sequences and heads                        */
+} intattn_append_args;
+
+/* Enqueues the append on hip_stream.  Allocates nothing. */
+INTATTN_API int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cache, const intattn_append_args *args,
+                                     void *hip_stream);
+
+/*
+ * The attention pipeline (steps 1 to 8 at the top of this file) for the newest tokens of each sequence over the cache: query
+ * token t of sequence b sees slots j <= lens[b] - n_new[b] + t, tokens from n_new[b] on are padding.  A row that sees no key
+ * comes out as zeros.  scale_q has a value for each token and head.  The output is INT8 as from intattn_forward, or
+ * P_hat . V_hat s_V / 255 in floating point.  With weight, each slot j < lens[b] of each KV head gets
+ *   weight_out = decay * weight + sum over the rows of its query heads and tokens of E_hat / rowSum(E_hat)
+ * in fp32 (slots behind stay as they are).
+ */
+typedef struct {
+    int32_t Hq, L;             /* query heads, a multiple of Hkv; query tokens of a sequence; Hq / Hkv * L <= 4096 */
+    int32_t max_len;           /* lens are taken as at most this, <= 131071; 0: max_pages * page_size        */
+    int32_t out_type;          /* 0 = fp32, 1 = fp16, 2 = bf16, 3 = INT8                                      */
+    const int8_t *q;           /* [B, Hq, L, d], BYTE strides multiples of 16                                */
+    int64_t q_stride[3];
+    const float *scale_q;      /* [B, Hq, L] contiguous                                                      */
+    const int32_t *n_new;      /* [B], taken as 0 .. min(L, lens[b]); NULL: min(L, lens[b])                  */
+    void *out;                 /* [B, Hq, L, d], BYTE strides multiples of 16                                */
+    int64_t out_stride[3];
+    const float *scale_out;    /* INT8 only: one value, or [Hq] in the cache's scale_mode 1; NULL: s_V       */
+    const float *weight;       /* optional [B, Hkv, slots]                                                   */
+    float *weight_out;         /* [B, Hkv, slots]; may be weight with the same strides                       */
+    int64_t weight_stride[2], weight_out_stride[2]; /* ELEMENTS between sequences and heads                  */
+    float decay;
+    int32_t reserved;          /* must be 0                                                                  */
+} intattn_cache_forward_args;
+
+/* Enqueues the attention on hip_stream.  Calls that need more room than the context has for the scores allocate it (a
+ * captured call is refused instead: intattn_cache_reserve first); room is never moved or given back before
+ * intattn_destroy.  Calls on one context must not overlap in time. */
+INTATTN_API int intattn_cache_forward(intattn_ctx *ctx, const intattn_cache *cache, const intattn_cache_forward_args *args,
+                                      void *hip_stream);
+
+/*
+ * Eviction by accumulated attention weight.  In each sequence with lens[b] > keep, every KV head loses the
+ * lens[b] - keep keys that come first by (held, weight, order, slot), where a key is held if its order is below sink or
+ * at least total[b] - recent (they leave last); NaN counts as the greatest weight.  The keys in slots from
+ * keep on that stay fill the gaps in front, the i-th key the i-th gap: K, V, weight and order of slots below keep are then those
+ * of the keys that stay.  lens_out[b] = min(lens[b], keep).  A sequence that has a page that is not there among its first
+ * lens[b] slots loses nothing, and lens_out[b] = lens[b].  weight_out and order_out are written up to slot lens_out[b];
+ * K and V in slots from keep on are left as they are, and their pages can be given back.
+ */
+typedef struct {
+    int32_t keep;              /* >= 1                                                                       */
+    int32_t sink, recent;      /* >= 0                                                                       */
+    int32_t max_len;           /* lens are taken as at most this, <= 131071; 0: max_pages * page_size        */
+    const float *weight;       /* [B, Hkv, slots]                                                            */
+    float *weight_out;         /* may be weight with the same strides                                        */
+    const int32_t *order;      /* [B, Hkv, slots], >= 0; NULL: the slot                                      */
+    int32_t *order_out;        /* may be order with the same strides; NULL if order is NULL                  */
+    int64_t weight_stride[2], weight_out_stride[2], order_stride[2], order_out_stride[2]; /* ELEMENTS, B and H */
+    const int32_t *total;      /* [B]; NULL: lens                                                            */
+    int32_t *lens_out;         /* [B]; may be lens                                                           */
+} intattn_evict_args;
+
+/* Enqueues the eviction on hip_stream; room as for intattn_cache_forward. */
+INTATTN_API int intattn_cache_evict(intattn_ctx *ctx, const intattn_cache *cache, const intattn_evict_args *args, void *hip_stream);
+
+/* Makes the room that calls on this cache with max_len (0: max_pages * page_size) need, so that they can be captured: rows > 0:
+ * intattn_cache_forward with up to that many rows Hq / Hkv * L a KV head; keep > 0: intattn_cache_evict to that many keys.
+ * May call hipMalloc; reads no device memory and launches nothing. */
+INTATTN_API int intattn_cache_reserve(intattn_ctx *ctx, const intattn_cache *cache, int32_t rows, int32_t keep, int32_t max_len);
 
 /* In-run comparator: the conventional INT8 pipeline the paper calls "Quant-Only"
  * (Sec. 2.2): INT8 Q.K^T, dequantize to fp32 with alpha, fp32 softmax, requantize P to

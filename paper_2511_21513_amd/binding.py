@@ -30,6 +30,11 @@ SYMBOLS = (
     "intattn_quantize",
     "intattn_quantize_batch",
     "intattn_index_softmax",
+    "intattn_rope",
+    "intattn_cache_append",
+    "intattn_cache_forward",
+    "intattn_cache_evict",
+    "intattn_cache_reserve",
     "intattn_derive_params",
     "intattn_derive_index_map",
     "intattn_kernel_choice",
@@ -94,6 +99,65 @@ class QuantArgs(ctypes.Structure):
     ]
 
 
+class Cache(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("scale_mode", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("lens", ctypes.c_void_p),
+        ("scale_k", ctypes.c_void_p), ("scale_v", ctypes.c_void_p),
+    ]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [
+        ("rot", ctypes.c_int32), ("pairing", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("inverse", ctypes.c_int32),
+        ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64 * 3), ("freq", ctypes.c_void_p), ("axis", ctypes.c_uint8 * 128),
+    ]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("H", ctypes.c_int32 * 2),
+        ("src", ctypes.c_void_p * 2), ("dst", ctypes.c_void_p * 2),
+        ("src_stride", (ctypes.c_int64 * 3) * 2), ("dst_stride", (ctypes.c_int64 * 3) * 2), ("rotary", Rotary),
+    ]
+
+
+class AppendArgs(ctypes.Structure):
+    _fields_ = [
+        ("L", ctypes.c_int32), ("Hq", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("n_new", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_out_stride", ctypes.c_int64 * 3), ("q_scale", ctypes.c_void_p),
+        ("rotary", Rotary), ("weight", ctypes.c_void_p), ("order", ctypes.c_void_p), ("first", ctypes.c_void_p),
+        ("weight_stride", ctypes.c_int64 * 2), ("order_stride", ctypes.c_int64 * 2),
+    ]
+
+
+class CacheForwardArgs(ctypes.Structure):
+    _fields_ = [
+        ("Hq", ctypes.c_int32), ("L", ctypes.c_int32), ("max_len", ctypes.c_int32), ("out_type", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 3), ("scale_q", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
+        ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64 * 3), ("scale_out", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p), ("weight_out", ctypes.c_void_p),
+        ("weight_stride", ctypes.c_int64 * 2), ("weight_out_stride", ctypes.c_int64 * 2),
+        ("decay", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class EvictArgs(ctypes.Structure):
+    _fields_ = [
+        ("keep", ctypes.c_int32), ("sink", ctypes.c_int32), ("recent", ctypes.c_int32), ("max_len", ctypes.c_int32),
+        ("weight", ctypes.c_void_p), ("weight_out", ctypes.c_void_p), ("order", ctypes.c_void_p), ("order_out", ctypes.c_void_p),
+        ("weight_stride", ctypes.c_int64 * 2), ("weight_out_stride", ctypes.c_int64 * 2),
+        ("order_stride", ctypes.c_int64 * 2), ("order_out_stride", ctypes.c_int64 * 2),
+        ("total", ctypes.c_void_p), ("lens_out", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 _F32 = np.dtype(np.float32)
 
@@ -125,6 +189,14 @@ def load() -> ctypes.CDLL:
         lib.intattn_dynamic_status.restype = ctypes.c_int
         lib.intattn_index_softmax.argtypes = [vp, ctypes.POINTER(SoftmaxArgs), vp]
         lib.intattn_index_softmax.restype = ctypes.c_int
+        cache = ctypes.POINTER(Cache)
+        lib.intattn_rope.argtypes = [vp, ctypes.POINTER(RopeArgs), vp]
+        lib.intattn_cache_append.argtypes = [vp, cache, ctypes.POINTER(AppendArgs), vp]
+        lib.intattn_cache_forward.argtypes = [vp, cache, ctypes.POINTER(CacheForwardArgs), vp]
+        lib.intattn_cache_evict.argtypes = [vp, cache, ctypes.POINTER(EvictArgs), vp]
+        lib.intattn_cache_reserve.argtypes = [vp, cache, i32, i32, i32]
+        for f in (lib.intattn_rope, lib.intattn_cache_append, lib.intattn_cache_forward, lib.intattn_cache_evict, lib.intattn_cache_reserve):
+            f.restype = i32
         lib.intattn_quantize.argtypes = [vp, ctypes.POINTER(QuantArgs), vp]
         lib.intattn_quantize.restype = i32
         lib.intattn_quantize_batch.argtypes = [vp, ctypes.POINTER(QuantArgs), i32, vp]
@@ -165,6 +237,74 @@ def _address(x):
         return ctypes.addressof(ctypes.c_char.from_buffer(x))
     except (TypeError, ValueError):
         return x.ctypes.data
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else 0
+
+
+def _check(t, what, dtype, shape, device, contiguous=False):
+    """A tensor (or None) that the struct will point at: its type, shape and place, which pointers do not carry."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device or len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+
+
+def _float_types():
+    import torch
+
+    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _slots(t, what, dtype, B, Hkv, slots, device):
+    """[B, Hkv, slots] planes: the last axis is contiguous and holds every slot the call may touch."""
+    _check(t, what, dtype, (B, Hkv, None), device)
+    if t is not None and (t.stride(2) != 1 or t.shape[2] < slots):
+        raise ValueError(f"{what} must hold {slots} slots, contiguous")
+    return t.stride()[:2] if t is not None else (0, 0)
+
+
+class PagedCache:
+    """A paged INT8 key/value cache (``intattn_cache``): the caller's tensors, checked once, and the struct that points at them.
+
+    ``k_pages``, ``v_pages``: int8 [n_pages, Hkv, page_size, d]; ``table``: int32 [B, max_pages], the pages of each sequence (a
+    number outside the pool: a page that is not there); ``lens``: int32 [B], keys of each sequence, which the caller keeps (in
+    place); ``scale_k``, ``scale_v``: float32, one value or one for each KV head.  The contents may change between calls."""
+
+    def __init__(self, k_pages, v_pages, table, lens, scale_k, scale_v):
+        import torch
+
+        dev = k_pages.device
+        if k_pages.dim() != 4 or not k_pages.is_cuda:
+            raise ValueError("k_pages must be an int8 tensor [n_pages, Hkv, page_size, d] on the GPU")
+        n_pages, Hkv, page, d = k_pages.shape
+        for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            _check(t, what, torch.int8, (n_pages, Hkv, page, d), dev)
+            if t.stride(3) != 1:
+                raise ValueError("the head dimension must be contiguous")
+        _check(table, "table", torch.int32, (None, None), dev)
+        if table.shape[1] > 1 and table.stride(1) != 1:
+            raise ValueError("rows of the table must be contiguous")
+        B = table.shape[0]
+        _check(lens, "lens", torch.int32, (B,), dev, True)
+        for t, what in ((scale_k, "scale_k"), (scale_v, "scale_v")):
+            _check(t, what, torch.float32, (scale_k.numel(),), dev, True)
+        if scale_k.numel() not in (1, Hkv):
+            raise ValueError("scales: one value, or one for each KV head")
+        self.k_pages, self.v_pages, self.table, self.lens, self.scale_k, self.scale_v = k_pages, v_pages, table, lens, scale_k, scale_v
+        self.B, self.Hkv, self.page_size, self.d, self.device = B, Hkv, page, d, dev
+        self.capacity = table.shape[1] * page
+        c = Cache()
+        c.B, c.Hkv, c.d, c.n_pages, c.page_size, c.max_pages = B, Hkv, d, n_pages, page, table.shape[1]
+        c.scale_mode = int(scale_k.numel() == Hkv)
+        c.k, c.v, c.table, c.lens = k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lens.data_ptr()
+        c.scale_k, c.scale_v = scale_k.data_ptr(), scale_v.data_ptr()
+        c.k_stride[:], c.v_stride[:] = k_pages.stride()[:3], v_pages.stride()[:3]
+        c.table_stride = table.stride(0)
+        self.args = c
 
 
 class IntAttn:
@@ -411,6 +551,194 @@ class IntAttn:
         if rc != OK:
             raise IntAttnError(rc, self.last_error())
         return outs, scales
+
+    def _stream(self, device, stream):
+        import torch
+
+        if device.index != self.device:
+            raise ValueError(f"tensors on {device}, context on device {self.device}")
+        return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream
+
+    @staticmethod
+    def _rotary(r, B, L, device, pos, freq, axis, pairing, inverse=False):
+        import torch
+
+        if pos.dim() == 2:
+            pos = pos[None]
+        _check(pos, "pos", torch.int32, (None, B, L), device)
+        _check(freq, "freq", torch.float64, (None,), device, True)
+        n = freq.shape[0]
+        if n > 128:
+            raise ValueError("at most 128 rotated pairs")
+        if pairing not in ("adjacent", "halves"):
+            raise ValueError("pairing is 'adjacent' or 'halves'")
+        r.rot, r.pairing, r.n_axes, r.inverse = 2 * n, int(pairing == "halves"), pos.shape[0], int(bool(inverse))
+        r.pos, r.freq = pos.data_ptr(), freq.data_ptr()
+        r.pos_stride[:] = pos.stride()
+        if axis is not None:
+            if len(axis) != n or min(axis) < 0 or max(axis) > 255:
+                raise ValueError("axis must name an axis for each pair")
+            r.axis[:n] = axis
+
+    def rope(self, x, pos, freq, *, axis=None, pairing="adjacent", inverse=False, out=None, stream=None):
+        """intattn_rope on a [B, H, L, d] tensor, or on two with the same B, L, d (Q and K): new tensors, or ``out``, which may be
+        ``x``.  ``pos``: int32 [axes, B, L] (or [B, L]); ``freq``: float64 [rot / 2], radians per position of each pair, on the
+        device; ``axis``: a list of each pair's axis (None: all the first).  ``inverse``: the gradient's rotation."""
+        import torch
+
+        one = torch.is_tensor(x)
+        xs = [x] if one else list(x)
+        if not 1 <= len(xs) <= 2:
+            raise ValueError("one tensor or two")
+        outs = [torch.empty_like(t) for t in xs] if out is None else [out] if torch.is_tensor(out) else list(out)
+        B, _, L, d = xs[0].shape
+        types, dev = _float_types(), xs[0].device
+        if xs[0].dtype not in types or len(outs) != len(xs):
+            raise ValueError("expected float32/float16/bfloat16 tensors and as many outputs")
+        a = RopeArgs()
+        a.B, a.L, a.d, a.dtype = B, L, d, types[xs[0].dtype]
+        es = xs[0].element_size()
+        for i, (t, o) in enumerate(zip(xs, outs)):
+            _check(t, "x", xs[0].dtype, (B, None, L, d), dev)
+            _check(o, "out", t.dtype, tuple(t.shape), dev)
+            if t.stride(3) != 1 or o.stride(3) != 1:
+                raise ValueError("the head dimension must be contiguous")
+            a.H[i], a.src[i], a.dst[i] = t.shape[1], t.data_ptr(), o.data_ptr()
+            for j in range(3):
+                a.src_stride[i][j], a.dst_stride[i][j] = t.stride(j) * es, o.stride(j) * es
+        self._rotary(a.rotary, B, L, dev, pos, freq, axis, pairing, inverse)
+        rc = self._lib.intattn_rope(self._ctx, ctypes.byref(a), ctypes.c_void_p(self._stream(dev, stream)))
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
+        return outs[0] if one else outs
+
+    def cache_append(self, cache: PagedCache, k, v, q=None, *, n_new=None, pos=None, freq=None, axis=None, pairing="adjacent",
+                     weight=None, order=None, first=None, q_out=None, q_scale=None, stream=None):
+        """intattn_cache_append: K and V [B, Hkv, L, d] of new tokens into the last slots of ``cache.lens`` (which already count
+        them), rotated if ``pos`` and ``freq`` are given (see ``rope``).  With Q [B, Hq, L, d]: returns its INT8 tensor and the scales
+        [B, Hq, L]."""
+        import torch
+
+        types, dev, B, L = _float_types(), cache.device, cache.B, k.shape[2]
+        if k.dtype not in types:
+            raise ValueError("expected float32/float16/bfloat16 tensors")
+        Hq = q.shape[1] if q is not None else 0
+        es = k.element_size()
+        a = AppendArgs()
+        a.L, a.Hq, a.dtype = L, Hq, types[k.dtype]
+        for t, what, h, at in ((q, "q", Hq, a.q_stride), (k, "k", cache.Hkv, a.k_stride), (v, "v", cache.Hkv, a.v_stride)):
+            if t is None:
+                continue
+            _check(t, what, k.dtype, (B, h, L, cache.d), dev)
+            st = t.stride()
+            if st[3] != 1:
+                raise ValueError("the head dimension must be contiguous")
+            at[0], at[1], at[2] = st[0] * es, st[1] * es, st[2] * es
+        a.k, a.v, a.q = k.data_ptr(), v.data_ptr(), _ptr(q)
+        _check(n_new, "n_new", torch.int32, (B,), dev, True)
+        a.n_new = _ptr(n_new)
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty((B, Hq, L, cache.d), dtype=torch.int8, device=dev)
+            if q_scale is None:
+                q_scale = torch.empty((B, Hq, L), dtype=torch.float32, device=dev)
+            _check(q_out, "q_out", torch.int8, (B, Hq, L, cache.d), dev)
+            _check(q_scale, "q_scale", torch.float32, (B, Hq, L), dev, True)
+            st = q_out.stride()
+            if st[3] != 1:
+                raise ValueError("the head dimension must be contiguous")
+            a.q_out, a.q_scale = q_out.data_ptr(), q_scale.data_ptr()
+            a.q_out_stride[:] = st[:3]
+        if pos is not None:
+            self._rotary(a.rotary, B, L, dev, pos, freq, axis, pairing)
+        if weight is not None or order is not None:
+            a.weight_stride[:] = _slots(weight, "weight", torch.float32, B, cache.Hkv, cache.capacity, dev)
+            a.order_stride[:] = _slots(order, "order", torch.int32, B, cache.Hkv, cache.capacity, dev)
+            _check(first, "first", torch.int32, (B,), dev, True)
+            a.weight, a.order, a.first = _ptr(weight), _ptr(order), _ptr(first)
+        rc = self._lib.intattn_cache_append(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(dev, stream)))
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
+        return (q_out, q_scale) if q is not None else None
+
+    def _cache_forward_args(self, cache, q, scale_q, out, dtype, scale_out, n_new, max_len, weight, weight_out, decay):
+        import torch
+
+        dev, (B, Hq, L, d) = cache.device, q.shape
+        _check(q, "q", torch.int8, (cache.B, Hq, L, cache.d), dev)
+        _check(scale_q, "scale_q", torch.float32, (B, Hq, L), dev, True)
+        _check(n_new, "n_new", torch.int32, (B,), dev, True)
+        a = CacheForwardArgs()
+        types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
+        if out is None:
+            out = torch.empty((B, Hq, L, d), dtype=dtype, device=dev)
+        _check(out, "out", out.dtype, (B, Hq, L, d), dev)
+        if out.dtype not in types or q.stride(3) != 1 or out.stride(3) != 1:
+            raise ValueError("out must be float32/float16/bfloat16/int8, the head dimension contiguous")
+        if scale_out is not None:
+            _check(scale_out, "scale_out", torch.float32, (Hq if cache.args.scale_mode else 1,), dev, True)
+        a.Hq, a.L, a.max_len, a.out_type = Hq, L, int(max_len), types[out.dtype]
+        es = out.element_size()
+        st, so = q.stride(), out.stride()
+        a.q_stride[:] = st[:3]
+        a.out_stride[0], a.out_stride[1], a.out_stride[2] = so[0] * es, so[1] * es, so[2] * es
+        a.q, a.scale_q, a.n_new, a.out, a.scale_out = q.data_ptr(), scale_q.data_ptr(), _ptr(n_new), out.data_ptr(), _ptr(scale_out)
+        if weight is not None:
+            slots = min(cache.capacity, max_len) if max_len else cache.capacity
+            weight_out = weight if weight_out is None else weight_out
+            a.weight_stride[:] = _slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev)
+            a.weight_out_stride[:] = _slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev)
+            a.weight, a.weight_out, a.decay = weight.data_ptr(), weight_out.data_ptr(), float(decay)
+        return a, out
+
+    def cache_forward(self, cache: PagedCache, q, scale_q, *, out=None, dtype=None, scale_out=None, n_new=None, max_len=0,
+                      weight=None, weight_out=None, decay=1.0, stream=None):
+        """intattn_cache_forward: INT8 queries [B, Hq, L, d] of the newest tokens, with a scale for each token and head, over the
+        cache.  Returns ``out`` (given, or new in ``dtype``; the default is torch.bfloat16, torch.int8 is the requantized form).  ``weight``
+        [B, Hkv, slots] float32: accumulated attention weight of each key, written to ``weight_out`` (default: in place)."""
+        import torch
+
+        a, out = self._cache_forward_args(cache, q, scale_q, out, dtype or torch.bfloat16, scale_out, n_new, max_len, weight, weight_out, decay)
+        rc = self._lib.intattn_cache_forward(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(cache.device, stream)))
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
+        return out
+
+    def _evict_args(self, cache, keep, weight, order, total, sink, recent, max_len, weight_out, order_out, lens_out):
+        import torch
+
+        dev, B, Hkv = cache.device, cache.B, cache.Hkv
+        slots = min(cache.capacity, max_len) if max_len else cache.capacity
+        weight_out = weight if weight_out is None else weight_out
+        order_out = order if order_out is None else order_out
+        lens_out = cache.lens if lens_out is None else lens_out
+        a = EvictArgs()
+        a.keep, a.sink, a.recent, a.max_len = int(keep), int(sink), int(recent), int(max_len)
+        for t, what, kind, at in ((weight, "weight", torch.float32, a.weight_stride), (weight_out, "weight_out", torch.float32, a.weight_out_stride),
+                                  (order, "order", torch.int32, a.order_stride), (order_out, "order_out", torch.int32, a.order_out_stride)):
+            at[0], at[1] = _slots(t, what, kind, B, Hkv, slots, dev)
+        _check(total, "total", torch.int32, (B,), dev, True)
+        _check(lens_out, "lens_out", torch.int32, (B,), dev, True)
+        a.weight, a.weight_out, a.order, a.order_out = _ptr(weight), _ptr(weight_out), _ptr(order), _ptr(order_out)
+        a.total, a.lens_out = _ptr(total), lens_out.data_ptr()
+        return a
+
+    def cache_evict(self, cache: PagedCache, keep: int, weight, *, order=None, total=None, sink=0, recent=0, max_len=0,
+                    weight_out=None, order_out=None, lens_out=None, stream=None):
+        """intattn_cache_evict: sequences longer than ``keep`` keep the keys of each head that have drawn most ``weight``
+        [B, Hkv, slots], among them the first ``sink`` and the last ``recent`` by ``order`` (int32 [B, Hkv, slots]; ``total`` [B]: tokens so
+        far).  weight, order and lens change in place unless ``*_out`` tensors are given."""
+        a = self._evict_args(cache, keep, weight, order, total, sink, recent, max_len, weight_out, order_out, lens_out)
+        rc = self._lib.intattn_cache_evict(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(cache.device, stream)))
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
+
+    def cache_reserve(self, cache: PagedCache, rows: int = 0, keep: int = 0, max_len: int = 0):
+        """intattn_cache_reserve: room for ``cache_forward`` with up to ``rows`` = Hq / Hkv * L rows a KV head and for ``cache_evict``
+        to ``keep`` keys, so that they can be captured."""
+        rc = self._lib.intattn_cache_reserve(self._ctx, ctypes.byref(cache.args), int(rows), int(keep), int(max_len))
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
 
     def forward_stage(self, args: Args, stage: int, stream: int = 0):
         """intattn_forward_stage: 0 = everything, 1 = sweeps A+B, 2 = sweep C."""

@@ -1,0 +1,104 @@
+// Parameters of the kernels around the paged cache.  Not part of the public ABI (that is include/intattn.h).
+#pragma once
+#include <stdint.h>
+
+#include "params.h"
+
+namespace intattn {
+
+struct CacheParams {
+    int8_t *k, *v;
+    int64_t ks[3], vs[3];      // bytes between pages, heads, keys
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *lens;
+    const float *scale_k, *scale_v;
+    int32_t B, Hkv;
+    int32_t n_pages, page_size, capacity; // capacity: the most slots a sequence is taken to have
+    int32_t per_head;
+    FastDiv by_page;           // of slot numbers by page_size
+};
+
+struct RotaryParams {
+    const int32_t *pos;
+    int64_t ps[3];
+    const double *freq;
+    int32_t rot, halves, inverse;
+    uint32_t axis[32];         // four axes of pairs to a word
+};
+
+struct RopeParams {
+    const uint8_t *src[2];
+    uint8_t *dst[2];
+    int64_t ss[2][3], ds[2][3];
+    int32_t H0, H;             // heads of the first tensor, of both
+    int32_t B, L, d;
+    int32_t tokens;            // of a workgroup
+    RotaryParams r;
+};
+
+struct AppendParams {
+    CacheParams c;
+    const uint8_t *x[3];       // q, k, v
+    int64_t xs[3][3];
+    int32_t Hq, L;
+    int32_t tokens;            // of a workgroup
+    const int32_t *n_new;
+    int8_t *q_out;
+    int64_t qos[3];
+    float *q_scale;
+    float *weight;
+    int32_t *order;
+    const int32_t *first;
+    int64_t wst[2], ost[2];
+    RotaryParams r;
+};
+
+struct AttendParams {
+    CacheParams c;
+    const int8_t *q;
+    int64_t qs[3];
+    const float *scale_q;
+    const int32_t *n_new;
+    uint8_t *out;
+    int64_t os[3];
+    const float *scale_out;
+    const float *weight;
+    float *weight_out;
+    int64_t wst[2], wost[2];
+    float decay;
+    int32_t Hq, L, group;      // group = Hq / Hkv
+    int32_t rows, blocks;      // group * L rows of a KV head, in blocks of 16
+    int32_t out_type;
+    int32_t top;
+    double clip, sqrt_d;
+    uint32_t lut[16];
+    int32_t *scores;           // room for scores that do not fit LDS: scores_step words for each step of 64 keys of a workgroup
+    int64_t scores_wg;         // words of a workgroup
+    int32_t lds_steps;         // steps of 64 keys whose scores LDS holds
+};
+
+struct EvictParams {
+    CacheParams c;
+    int32_t keep, sink, recent;
+    const float *weight;
+    float *weight_out;
+    const int32_t *order;
+    int32_t *order_out;
+    int64_t wst[2], wost[2], ost[2], oost[2];
+    const int32_t *total;
+    int32_t *lens_out;
+    int32_t *count;            // room: moves of each (sequence, KV head), and then the new length of each sequence
+    int32_t *moves;            // room: [B * Hkv][2][max_moves], the slots to fill and the slots to fill them from
+    int32_t max_moves, d;
+};
+
+int launch_rope(const RopeParams &p, int dtype, void *stream);
+int launch_append(const AppendParams &p, int d, int dtype, void *stream);
+// bytes of room that launch_attend needs for these parameters
+int64_t attend_room(const AttendParams &p, int d);
+int launch_attend(const AttendParams &p, int d, void *room, void *stream);
+int64_t evict_room(const EvictParams &p);
+int launch_evict(const EvictParams &p, void *room, void *stream);
+
+} // namespace intattn
