@@ -343,12 +343,12 @@ typedef struct {
     const int32_t *n_new;      /* [B], taken as 0 .. min(L, lens[b]); NULL: min(L, lens[b])                  */
     void *out;                 /* [B, Hq, L, d], BYTE strides multiples of 16                                */
     int64_t out_stride[3];
-    const float *scale_out;    /* INT8 only: one value, or [Hq] in the cache's scale_mode 1; NULL: s_V       */
+    const float *scale_out;    /* INT8 only: one value (scale_out_mode 0) or [Hq] (1); NULL: s_V             */
     const float *weight;       /* optional [B, Hkv, slots]                                                   */
     float *weight_out;         /* [B, Hkv, slots]; may be weight with the same strides                       */
     int64_t weight_stride[2], weight_out_stride[2]; /* ELEMENTS between sequences and heads                  */
     float decay;
-    int32_t reserved;          /* must be 0                                                                  */
+    int32_t scale_out_mode;
 } intattn_cache_forward_args;
 
 /* Enqueues the attention on hip_stream.  Calls that need more room than the context has for the scores allocate it (a

@@ -144,7 +144,7 @@ class CacheForwardArgs(ctypes.Structure):
         ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64 * 3), ("scale_out", ctypes.c_void_p),
         ("weight", ctypes.c_void_p), ("weight_out", ctypes.c_void_p),
         ("weight_stride", ctypes.c_int64 * 2), ("weight_out_stride", ctypes.c_int64 * 2),
-        ("decay", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("decay", ctypes.c_float), ("scale_out_mode", ctypes.c_int32),
     ]
 
 
@@ -676,7 +676,8 @@ class IntAttn:
         if out.dtype not in types or q.stride(3) != 1 or out.stride(3) != 1:
             raise ValueError("out must be float32/float16/bfloat16/int8, the head dimension contiguous")
         if scale_out is not None:
-            _check(scale_out, "scale_out", torch.float32, (Hq if cache.args.scale_mode else 1,), dev, True)
+            a.scale_out_mode = int(scale_out.numel() > 1)
+            _check(scale_out, "scale_out", torch.float32, (Hq if a.scale_out_mode else 1,), dev, True)
         a.Hq, a.L, a.max_len, a.out_type = Hq, L, int(max_len), types[out.dtype]
         es = out.element_size()
         st, so = q.stride(), out.stride()

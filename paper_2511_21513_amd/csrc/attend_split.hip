@@ -1,0 +1,324 @@
+// Attention of the newest tokens over a paged INT8 cache with the keys of a (sequence, KV head) split over workgroups, for gfx950: for long
+// sequences, and for batches of any lengths.  IndexSoftmax is exact in the row maximum and the row sum, and partial results of other
+// maxima cannot be joined afterwards, so the work is cut at both, each a launch boundary: no workgroup waits for another.
+//   scores   Q.K^T of a chunk of keys: INT32 scores to room of the context, a maximum for each row and chunk
+//   lookup   the row's maximum; scores become table indices (a byte each, in place), a sum for each row and chunk
+//   values   the row's sum; P.V of a chunk; the last workgroup of a KV head's chunks adds them up and writes the rows
+// K and V are read once, and the scores (4 bytes for each row and key against 2 d for a key) mostly stay in the caches between the
+// launches.  The chunks of all sequences are one grid of small workgroups, which evens out sequences of different lengths.
+//
+// Scores of a step of 64 keys: [ii][row][kb] of four keys 16 kb + 4 ii each, so that a wave's stores are contiguous; the sixteen
+// indices of (row, kb) take the place of its first four scores.
+#include "attend_common.h"
+
+namespace intattn {
+
+namespace {
+
+constexpr int SNT = 256, SWAVES = 4;
+constexpr int SBLK = 8, SROWS = 16 * SBLK; // rows of a workgroup in the first two launches
+
+struct Group {
+    int b, kvh, len, fresh, steps;
+};
+__device__ __forceinline__ Group group_of(const AttendParams &p, int g)
+{
+    Group r;
+    r.b = g / p.c.Hkv;
+    r.kvh = g % p.c.Hkv;
+    r.len = cache_len(p.c, r.b);
+    r.fresh = new_tokens(p.n_new, r.b, p.L, r.len);
+    r.steps = (r.len + 63) / 64;
+    return r;
+}
+// slots that a row sees, whatever its scale
+__device__ __forceinline__ int row_limit(const AttendParams &p, const Group &g, int row)
+{
+    const int t = row % p.L;
+    return row < p.rows && t < g.fresh ? g.len - g.fresh + t + 1 : 0;
+}
+__device__ __forceinline__ int4 *step_of(const AttendParams &p, int g, int s) { return (int4 *)p.scores + ((int64_t)g * p.steps + s) * 16 * p.rows; }
+
+template <int D, bool WHOLE, bool ONE> __global__ __launch_bounds__(SNT) void cache_scores_kernel(const AttendParams p)
+{
+    constexpr int KB = D / 64;
+    __shared__ int limit[SROWS], most[SROWS];
+    __shared__ v4i q_lds[ONE ? 1 : SBLK][KB][64];
+    const int chunk = blockIdx.x, g = blockIdx.y, blk0 = blockIdx.z * SBLK;
+    const Group gr = group_of(p, g);
+    const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
+    if (s0 >= s1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int blocks = ONE ? 1 : min(SBLK, p.blocks - blk0);
+    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1], gr.len};
+    v4i qf[KB];
+    if constexpr (ONE) {
+        load_q<D>(p, gr.b, gr.kvh, n, kb, qf);
+    } else {
+        for (int i = wave; i < blocks; i += SWAVES) {
+            load_q<D>(p, gr.b, gr.kvh, (blk0 + i) * 16 + n, kb, qf);
+#pragma unroll
+            for (int j = 0; j < KB; ++j) q_lds[i][j][lane] = qf[j];
+        }
+    }
+    for (int i = threadIdx.x; i < blocks * 16; i += SNT) {
+        limit[i] = row_limit(p, gr, blk0 * 16 + i);
+        most[i] = HIDDEN;
+    }
+    __syncthreads();
+    for (int s = s0 + wave; s < s1; s += SWAVES) {
+        v4i a[4][KB];
+        bool there[4];
+        keys.load_k(s, lane, a, there);
+        int4 *const to = step_of(p, g, s);
+        for (int i = 0; i < blocks; ++i) {
+            if constexpr (!ONE) {
+#pragma unroll
+                for (int j = 0; j < KB; ++j) qf[j] = q_lds[i][j][lane];
+            }
+            v4i sc[4];
+            step_scores<D>(a, there, qf, limit[i * 16 + n] - (s * 64 + 16 * kb), kb, sc);
+            int top = HIDDEN;
+            const int row = (blk0 + i) * 16 + n;
+#pragma unroll
+            for (int ii = 0; ii < 4; ++ii) {
+                top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
+                if (row < p.rows) to[(ii * p.rows + row) * 4 + kb] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
+            }
+            top = max(top, __shfl_xor(top, 16));
+            top = max(top, __shfl_xor(top, 32));
+            if (kb == 0) atomicMax(&most[i * 16 + n], top);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < blocks * 16; i += SNT) {
+        const int row = blk0 * 16 + i;
+        if (row < p.rows) p.part_max[((int64_t)g * p.chunks + chunk) * p.rows + row] = most[i];
+    }
+}
+
+__global__ __launch_bounds__(SNT) void cache_lookup_kernel(const AttendParams p)
+{
+    __shared__ RowParams rowp[SROWS];
+    __shared__ int most[SROWS], total[SROWS];
+    __shared__ uint8_t entry[64];
+    const int chunk = blockIdx.x, g = blockIdx.y, row0 = blockIdx.z * SROWS, rows = min(SROWS, p.rows - row0);
+    const Group gr = group_of(p, g);
+    const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
+    if (chunk == 0) // arrivals of the next launch
+        for (int i = threadIdx.x; i < (rows + 15) / 16; i += SNT) p.arrived[g * p.blocks + row0 / 16 + i] = 0;
+    if (s0 >= s1) return;
+    const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
+    if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
+    for (int i = threadIdx.x; i < rows; i += SNT) {
+        most[i] = HIDDEN;
+        total[i] = 0;
+        const int row = row0 + i;
+        RowParams rp;
+        const bool ok = row_params(p, gr.b, gr.kvh * p.group + row / p.L, row % p.L, gr.kvh, rp);
+        rp.limit = ok;
+        rowp[i] = rp;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * live; i += SNT)
+        atomicMax(&most[i % rows], p.part_max[((int64_t)g * p.chunks + i / rows) * p.rows + row0 + i % rows]);
+    __syncthreads();
+    const int per_step = rows * 4;
+    for (int i = threadIdx.x; i < (s1 - s0) * per_step; i += SNT) {
+        const int s = i / per_step, at = i % per_step, r = at / 4;
+        int4 *const from = step_of(p, g, s0 + s) + row0 * 4 + at;
+        int4 x[4];
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) x[ii] = from[ii * p.rows * 4];
+        const RowParams rp = rowp[r];
+        const int top = most[r];
+        int sum = 0;
+        uint32_t word[4];
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(x[ii], top, rp, entry, sum);
+        from[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+        atomicAdd(&total[r], sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows; i += SNT) // a row that sees nothing, or has no scale: 0
+        p.part_sum[((int64_t)g * p.chunks + chunk) * p.rows + row0 + i] = most[i] == HIDDEN || !rowp[i].limit ? 0 : total[i];
+}
+
+// P_hat and E / S of each index for 16 rows from row0 on; S = 0: zeros
+__device__ __forceinline__ void row_tables(const AttendParams &p, int g, int row0, int live, uint8_t (*prob)[64], float (*share)[64])
+{
+    const int r = threadIdx.x >> 4, part = threadIdx.x & 15, row = row0 + r;
+    int sum = 0;
+    if (row < p.rows)
+        for (int c = part; c < live; c += 16) sum += p.part_sum[((int64_t)g * p.chunks + c) * p.rows + row];
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) sum += __shfl_xor(sum, o);
+    const uint32_t S = (uint32_t)max(sum, 1);
+    const float inv = __builtin_amdgcn_rcpf((float)(2u * S));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int idx = 4 * part + i;
+        const uint32_t e = sum > 0 ? (p.lut[part] >> (8 * i)) & 0xffu : 0u;
+        prob[r][idx] = (uint8_t)prob_u8(e, S, inv);
+        if (share) share[r][idx] = (float)e / (float)S;
+    }
+}
+
+template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void cache_values_kernel(const AttendParams p)
+{
+    constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1;
+    __shared__ uint8_t prob[16][64];
+    __shared__ float share[WEIGHT ? 16 : 1][64];
+    __shared__ int acc_sum[16 * ACC_ROW];
+    __shared__ int last;
+    const int chunk = blockIdx.x, g = blockIdx.y, blk = blockIdx.z;
+    const Group gr = group_of(p, g);
+    const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
+    if (chunk > 0 && s0 >= s1) return;
+    const int live = max((gr.steps + p.chunk_steps - 1) / p.chunk_steps, 1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4, row = blk * 16 + n;
+    const int rows = min(16, p.rows - blk * 16);
+    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1], gr.len};
+    row_tables(p, g, blk * 16, gr.steps > 0 ? live : 0, prob, WEIGHT ? share : nullptr);
+    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += SNT) acc_sum[i] = 0;
+    __syncthreads();
+    const bool mine = n < rows;
+    v4i acc[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
+    for (int s = s0 + wave; s < s1; s += SWAVES) {
+        uint32_t v[16][KB];
+        keys.load_v(s, lane, v);
+        int4 x = make_int4(0, 0, 0, 0);
+        if (mine) x = step_of(p, g, s)[row * 4 + kb];
+        const uint32_t word[4] = {(uint32_t)x.x, (uint32_t)x.y, (uint32_t)x.z, (uint32_t)x.w};
+        v4i pf = {0, 0, 0, 0};
+        float w[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t idx = (word[j / 4] >> (8 * (j & 3))) & 0xffu;
+            const uint32_t pr = mine ? prob[n][idx] : 0u;
+            pf[j / 4] |= (int)(pr << (8 * (j & 3)));
+            if constexpr (WEIGHT) w[j] = mine ? share[n][idx] : 0.0f;
+        }
+        step_pv<D>(v, pf, acc);
+        if constexpr (WEIGHT) {
+            const float drawn = scatter_sum16(w, n);
+            const int slot = s * 64 + 16 * kb + n;
+            if (slot < gr.len)
+                p.weight_out[gr.b * p.wost[0] + gr.kvh * p.wost[1] + slot] = p.decay * p.weight[gr.b * p.wst[0] + gr.kvh * p.wst[1] + slot] + drawn;
+        }
+    }
+    if (mine) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
+    }
+    __syncthreads();
+    int32_t *const part = p.part_acc + ((int64_t)g * p.blocks + blk) * p.chunks * 16 * D;
+    if (live > 1) {
+        // device-scope stores and loads for what another workgroup reads: they pass the L2 of the XCD
+        for (int i = threadIdx.x; i < rows * D; i += SNT)
+            __hip_atomic_store(part + (int64_t)chunk * 16 * D + i, acc_sum[i / D * ACC_ROW + i % D], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) last = (int)atomicAdd((unsigned *)&p.arrived[g * p.blocks + blk], 1u);
+        __syncthreads();
+        if (last != live - 1) return;
+    }
+    for (int i = threadIdx.x; i < rows * D; i += SNT) {
+        const int r = i / D, ch = i % D, out = blk * 16 + r;
+        int sum = 0;
+        if (live > 1) {
+            for (int c = 0; c < live; ++c) sum += __hip_atomic_load(part + (int64_t)c * 16 * D + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        } else {
+            sum = acc_sum[r * ACC_ROW + ch];
+        }
+        RowParams rp;
+        if (!row_params(p, gr.b, gr.kvh * p.group + out / p.L, out % p.L, gr.kvh, rp)) sum = 0;
+        store_out(p, rp, out_row(p, gr.b, gr.kvh, out), ch, sum);
+    }
+}
+
+// Weights where a KV head has more than 16 rows: a thread for each key, over all rows.
+__global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p)
+{
+    __shared__ uint8_t prob[16][64];
+    __shared__ float share[16][64];
+    const int g = blockIdx.y;
+    const Group gr = group_of(p, g);
+    const int slot = blockIdx.x * SNT + threadIdx.x;
+    if ((int)blockIdx.x * SNT >= gr.len) return;
+    const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
+    const bool mine = slot < gr.len;
+    float drawn = 0.0f;
+    for (int blk = 0; blk < p.blocks; ++blk) {
+        __syncthreads();
+        row_tables(p, g, blk * 16, live, prob, share);
+        __syncthreads();
+        const int rows = min(16, p.rows - blk * 16);
+        if (mine) {
+            const uint8_t *at = (const uint8_t *)(step_of(p, g, slot >> 6) + blk * 16 * 4) + (slot & 63);
+            for (int r = 0; r < rows; ++r) drawn += share[r][at[64 * r]];
+        }
+    }
+    if (mine) p.weight_out[gr.b * p.wost[0] + gr.kvh * p.wost[1] + slot] = p.decay * p.weight[gr.b * p.wst[0] + gr.kvh * p.wst[1] + slot] + drawn;
+}
+
+} // namespace
+
+static void plan(AttendParams &p)
+{
+    p.steps = (p.c.capacity + 63) / 64;
+    const int64_t all = (int64_t)p.steps * p.c.B * p.c.Hkv;
+    int64_t c = (all + 4095) / 4096;          // about 4096 workgroups, of a step for each wave at least
+    if (c < (p.steps + 63) / 64) c = (p.steps + 63) / 64; // and at most 64 chunks of a sequence
+    p.chunk_steps = (int32_t)((c + SWAVES - 1) / SWAVES * SWAVES);
+    p.chunks = (p.steps + p.chunk_steps - 1) / p.chunk_steps;
+}
+
+int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParams *out)
+{
+    AttendParams p = p_;
+    plan(p);
+    const int64_t groups = (int64_t)p.c.B * p.c.Hkv;
+    int64_t at = 0;
+    auto take = [&](int64_t words) {
+        int32_t *const m = room ? (int32_t *)room + at : nullptr;
+        at += (words + 63) / 64 * 64;
+        return m;
+    };
+    p.scores = take(groups * p.steps * 64 * p.rows);
+    p.part_max = take(groups * p.chunks * p.rows);
+    p.part_sum = take(groups * p.chunks * p.rows);
+    p.part_acc = take(groups * p.blocks * p.chunks * 16 * d);
+    p.arrived = take(groups * p.blocks);
+    if (out) *out = p;
+    return 4 * at;
+}
+
+template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, hipStream_t st)
+{
+    const uint32_t groups = (uint32_t)(p.c.B * p.c.Hkv), supers = (uint32_t)((p.rows + SROWS - 1) / SROWS);
+    if (p.blocks == 1) hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, true>), dim3((uint32_t)p.chunks, groups, 1), dim3(SNT), 0, st, p);
+    else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.chunks, groups, supers), dim3(SNT), 0, st, p);
+    hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.chunks, groups, supers), dim3(SNT), 0, st, p);
+    const bool inside = p.weight && p.blocks == 1;
+    hipLaunchKernelGGL((inside ? cache_values_kernel<D, WHOLE, true> : cache_values_kernel<D, WHOLE, false>), dim3((uint32_t)p.chunks, groups, (uint32_t)p.blocks),
+                       dim3(SNT), 0, st, p);
+    if (p.weight && !inside) hipLaunchKernelGGL(cache_weights_kernel, dim3((uint32_t)((p.c.capacity + SNT - 1) / SNT), groups), dim3(SNT), 0, st, p);
+}
+
+int launch_attend_split(const AttendParams &p_, int d, void *room, void *stream)
+{
+    AttendParams p;
+    attend_split_room(p_, d, room, &p);
+    const bool whole = p.c.page_size % 16 == 0;
+    hipStream_t st = (hipStream_t)stream;
+    if (d == 64) whole ? launch_split_d<64, true>(p, st) : launch_split_d<64, false>(p, st);
+    else whole ? launch_split_d<128, true>(p, st) : launch_split_d<128, false>(p, st);
+    return (int)hipGetLastError();
+}
+
+} // namespace intattn

@@ -154,7 +154,7 @@ int forward_params(intattn_ctx *ctx, const intattn_cache *cache, const intattn_c
     rc = bound_len(ctx, a->max_len, &p->c);
     if (rc) return rc;
     if (a->out_type < 0 || a->out_type > 3) return fail(ctx, INTATTN_ERR_INVALID_ARG, "out_type must be 0 (fp32), 1 (fp16), 2 (bf16) or 3 (INT8)");
-    if (a->reserved != 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "reserved must be 0");
+    if (a->scale_out_mode != 0 && a->scale_out_mode != 1) return fail(ctx, INTATTN_ERR_INVALID_ARG, "scale_out_mode must be 0 or 1");
     if (!a->q || !a->scale_q || !a->out) return fail(ctx, INTATTN_ERR_INVALID_ARG, "q, scale_q, out must be non-NULL");
     if (!aligned(a->q, 16) || !aligned(a->out, 16) || !strides_ok(a->q_stride, 3, 16) || !strides_ok(a->out_stride, 3, 16))
         return fail(ctx, INTATTN_ERR_INVALID_ARG, "q, out and their strides must be multiples of 16");
@@ -172,6 +172,7 @@ int forward_params(intattn_ctx *ctx, const intattn_cache *cache, const intattn_c
     p->out = (uint8_t *)a->out;
     for (int i = 0; i < 3; ++i) { p->qs[i] = a->q_stride[i]; p->os[i] = a->out_stride[i]; }
     p->scale_out = a->out_type == 3 ? a->scale_out : nullptr;
+    p->out_per_head = a->scale_out_mode;
     p->weight = a->weight; p->weight_out = a->weight_out;
     for (int i = 0; i < 2; ++i) { p->wst[i] = a->weight_stride[i]; p->wost[i] = a->weight_out_stride[i]; }
     p->decay = a->decay;
@@ -381,6 +382,7 @@ int intattn_cache_reserve(intattn_ctx *ctx, const intattn_cache *cache, int32_t 
             std::memset(&p, 0, sizeof(p));
             p.c = c;
             p.rows = rows;
+            p.blocks = (rows + 15) / 16;
             bytes = std::max(bytes, attend_room(p, cache->d));
         }
         if (keep > 0) {

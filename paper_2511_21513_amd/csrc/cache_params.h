@@ -63,6 +63,7 @@ struct AttendParams {
     uint8_t *out;
     int64_t os[3];
     const float *scale_out;
+    int32_t out_per_head;
     const float *weight;
     float *weight_out;
     int64_t wst[2], wost[2];
@@ -76,6 +77,11 @@ struct AttendParams {
     int32_t *scores;           // room for scores that do not fit LDS: scores_step words for each step of 64 keys of a workgroup
     int64_t scores_wg;         // words of a workgroup
     int32_t lds_steps;         // steps of 64 keys whose scores LDS holds
+    // keys split over workgroups (attend_split.hip): chunks of chunk_steps steps, `chunks` of them and `steps` steps where a
+    // sequence has capacity slots.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks][rows], accumulators
+    // [group][block of rows][chunks][16][d], arrivals [group][block of rows]; a group is a (sequence, KV head)
+    int32_t steps, chunks, chunk_steps;
+    int32_t *part_max, *part_sum, *part_acc, *arrived;
 };
 
 struct EvictParams {
@@ -98,6 +104,8 @@ int launch_append(const AppendParams &p, int d, int dtype, void *stream);
 // bytes of room that launch_attend needs for these parameters
 int64_t attend_room(const AttendParams &p, int d);
 int launch_attend(const AttendParams &p, int d, void *room, void *stream);
+int64_t attend_split_room(const AttendParams &p, int d, void *room, AttendParams *out);
+int launch_attend_split(const AttendParams &p, int d, void *room, void *stream);
 int64_t evict_room(const EvictParams &p);
 int launch_evict(const EvictParams &p, void *room, void *stream);
 

@@ -160,6 +160,9 @@ FORWARDS = [
     (1, 35, 5, 64, 100, 5, [260], [3], False),         # 35 rows a head, seven heads of one
     (2, 3, 3, 128, 16, 1, [1500, 700], None, True),
     (1, 16, 2, 64, 7, 2, [555], None, True),
+    (5, 4, 2, 128, 64, 1, [2100, 0, 1, 1025, 64], None, True),   # long, none, one and a step in a batch
+    (2, 20, 1, 64, 16, 2, [1300, 3], [2, 1], False),
+    (3, 3, 3, 64, 24, 4, [1500, 2, 600], [4, 0, 3], True),
 ]
 
 
@@ -242,23 +245,32 @@ def test_forward_lengths_are_kept_inside_the_table(torch, ia):
     assert int((got.cpu().numpy() != want[1]).sum()) == 0
     got, wt, want, w = run_forward(torch, ia, c, 2, 2, [1, -3, 5, 2], max_len=37)
     assert int((got.cpu().numpy() != want[1]).sum()) == 0
+    c = Case(torch, 32, 3, 1, 64, 16, [1200, 1200, 1200], room=0)
+    c.lens = np.array([-5, 1201, 2 ** 31 - 1], dtype=np.int32)
+    c.up(torch)
+    got, wt, want, w = run_forward(torch, ia, c, 2, 1, None)
+    assert int((got.cpu().numpy() != want[1]).sum()) == 0
 
 
 @pytest.mark.parametrize("bad", [0.0, -1.0, math.inf, math.nan])
-def test_forward_unusable_scales_give_zeros(torch, ia, bad):
-    c = Case(torch, 41, 2, 2, 64, 16, [33, 50])
+@pytest.mark.parametrize("room", [1, 80])  # the table's width says how long a sequence may be
+def test_forward_unusable_scales_give_zeros(torch, ia, bad, room):
+    c = Case(torch, 41, 2, 2, 64, 16, [33, 50], room=room)
     q, s, qt, st = c.queries(torch, 4, 1)
     s[0, 1], s[1, 2] = bad, bad
     got = ia.cache_forward(c.cache, qt, dev(torch, s), dtype=torch.int8)
     assert int((got.cpu().numpy() != plain.attend(q, s, c.k, c.v, c.table, c.lens, c.sk, c.sv)[1]).sum()) == 0
     assert int(got[0, 1].abs().sum()) == 0
-    c.sk[1] = bad
-    c.up(torch)
-    got = ia.cache_forward(c.cache, qt, st, dtype=torch.float32)
-    assert int((got[:, 2:] != 0).sum()) == 0 and int((got[:, :2] != 0).sum()) > 0
+    for name in ("sk", "sv"):
+        was = getattr(c, name).copy()
+        getattr(c, name)[1] = bad
+        c.up(torch)
+        got = ia.cache_forward(c.cache, qt, st, dtype=torch.float32)
+        assert int((got[:, 2:] != 0).sum()) == 0 and int((got[:, :2] != 0).sum()) > 0
+        setattr(c, name, was)
 
 
-@pytest.mark.parametrize("rows, d, page, n", [(16, 64, 16, 2300), (4, 128, 64, 9001), (1, 64, 24, 40000), (33, 128, 128, 2500)])
+@pytest.mark.parametrize("rows, d, page, n", [(16, 64, 16, 2300), (4, 128, 64, 9001), (1, 64, 24, 40000), (33, 128, 128, 2500), (150, 64, 16, 1100), (2, 128, 1, 1030)])
 def test_forward_of_long_sequences(torch, ia, rows, d, page, n):
     """Scores past what the kernels keep close by; every key counts."""
     c = Case(torch, rows, 1, 1, d, page, [n], room=0)

@@ -135,7 +135,7 @@ def test_caches_that_are_refused(ia, want, kw):
 
 @pytest.mark.parametrize("want, kw", [
     (BAD, dict(Hq=0)), (BAD, dict(L=0)), (BAD, dict(Hq=6)), (NOT, dict(L=2049)), (BAD, dict(max_len=-1)), (BAD, dict(out_type=4)), (BAD, dict(out_type=-1)),
-    (BAD, dict(reserved=3)), (BAD, dict(q=None)), (BAD, dict(scale_q=None)), (BAD, dict(out=None)), (BAD, dict(q=P + 8)), (BAD, dict(out=P + 4)), (BAD, dict(q_stride=(1, 40))),
+    (BAD, dict(scale_out_mode=2)), (BAD, dict(scale_out_mode=-1)), (BAD, dict(q=None)), (BAD, dict(scale_q=None)), (BAD, dict(out=None)), (BAD, dict(q=P + 8)), (BAD, dict(out=P + 4)), (BAD, dict(q_stride=(1, 40))),
     (BAD, dict(out_stride=(2, 72))), (BAD, dict(scale_q=P + 2)), (BAD, dict(n_new=P + 1)), (BAD, dict(weight=None)), (BAD, dict(weight_out=None)), (BAD, dict(weight_stride=(0, -4))),
     (BAD, dict(weight_out_stride=(1, 81))), (BAD, dict(decay=float("nan"))), (BAD, dict(decay=float("inf"))),
 ])
