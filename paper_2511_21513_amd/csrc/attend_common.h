@@ -11,15 +11,8 @@ namespace intattn {
 
 namespace {
 
+constexpr int PROB = 68; // bytes of a row's probabilities in LDS: rows start in banks of their own
 constexpr int HIDDEN = (int)0x80000000; // further below any row maximum than any clip threshold
-
-struct RowParams {
-    double factor;   // the double after top / c_int
-    float unit;      // floating-point output of one step of the accumulator
-    int32_t c_int;
-    int32_t limit;   // slots that the row sees
-    int32_t mult, shift;
-};
 
 // c_int, index factor and output of one row, with the host's arithmetic; false where a scale is unusable
 __device__ __forceinline__ bool row_params(const AttendParams &p, int b, int head, int t, int kvh, RowParams &rp)
@@ -70,93 +63,109 @@ __device__ __forceinline__ void transpose4(const uint32_t w0, const uint32_t w1,
     o[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
-// Where lanes find their keys.  WHOLE: pages of a multiple of 16 keys, so that 16 keys from a multiple of 16 on lie in one.
-// Keys past the end, and keys of pages that are not there, are read from the pool's first row (their probability is 0).
+// Where lanes find their keys.  WHOLE: pages of a multiple of 16 keys whose rows follow each other, so that 16 keys from a multiple of 16
+// on are one run of 16 d bytes: one look into the table, and offsets that are part of the instruction (with a stride that is not known
+// the sixteen addresses of a step of V took 32 registers).  Keys past the end are read where the table says, which does not wait for
+// the length, and keys of pages that are not there from the pool's first page (the probability of either is 0).  V is read once and in whole lines, past the caches (8 KiB blocks in no order: 6.1 TB/s,
+// 5.4 through them); half lines of K need the cache.
+//
+// find_*() asks the table, load_*() for the keys.  They are apart so that a loop can ask for the places of a step before it asks for the
+// keys of an earlier one: loads come back in order, and a place asked for last could only be waited for together with every key
+// that is on its way.  (Scalar loads, which are counted apart, miss their cache too often: 4.6 -> 6.4 us for the first launch on 700 keys.)
 template <int D, bool WHOLE> struct Keys {
     const CacheParams &c;
     const int32_t *row;
     int64_t head_k, head_v;
-    int n; // slots in use
 
-    __device__ __forceinline__ Slot at(int slot) const
+    struct Place {
+        int entry, at; // of the table, as it is; place in the page
+    };
+    struct PlaceK {
+        Place p[WHOLE ? 1 : 4];
+    };
+    __device__ __forceinline__ Place find(int slot) const
     {
-        if (slot >= n) return Slot{-1, 0};
-        const Slot s = find_slot(c, row, slot);
-        return s.page < 0 ? Slot{-1, 0} : s;
+        slot = min(slot, c.capacity - 1);
+        const int n = quotient(slot, c.by_page);
+        return Place{row[n], slot - n * c.page_size};
     }
-    // 16 bytes of each of the lane's four keys 4 m + i of the step, channels 16 kb + 64 j on; there[i]: the key's page is there
-    __device__ __forceinline__ void load_k(int step, int lane, v4i (&a)[4][D / 64], bool (&there)[4]) const
+    __device__ __forceinline__ bool there(const Place &p) const { return (uint32_t)p.entry < (uint32_t)c.n_pages; }
+    // the lane's four keys 4 m + i of the step
+    __device__ __forceinline__ PlaceK find_k(int step, int lane) const
     {
-        const int m = lane & 15, kb = lane >> 4;
-        Slot s[4];
-        if constexpr (WHOLE) {
-            s[0] = at(step * 64 + 4 * m);
+        PlaceK k;
 #pragma unroll
-            for (int i = 1; i < 4; ++i) s[i] = Slot{s[0].page, s[0].at + i};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = at(step * 64 + 4 * m + i);
-        }
+        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) k.p[i] = find(step * 64 + 4 * (lane & 15) + i);
+        return k;
+    }
+    // the lane's sixteen keys from 16 kb on; not WHOLE: key 16 kb + m of them
+    __device__ __forceinline__ Place find_v(int step, int lane) const { return find(step * 64 + 16 * (lane >> 4) + (WHOLE ? 0 : lane & 15)); }
+
+    // 16 bytes of each of the lane's four keys, channels 16 kb + 64 j on; is[i]: the key's page is there
+    __device__ __forceinline__ void load_k(const PlaceK &k, int lane, v4i (&a)[4][D / 64], bool (&is)[4]) const
+    {
+        const int kb = lane >> 4;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            there[i] = s[i].page >= 0;
-            const int8_t *at_ = c.k + head_k + max(s[i].page, 0) * c.ks[0] + s[i].at * c.ks[2] + 16 * kb;
+            const Place &p = k.p[WHOLE ? 0 : i];
+            is[i] = there(p);
+            const int8_t *from = c.k + head_k + (is[i] ? p.entry : 0) * c.ks[0] + (is[i] ? p.at : 0) * (WHOLE ? D : c.ks[2]) + 16 * kb + (WHOLE ? i * D : 0);
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) a[i][j] = *(const v4i *)(at_ + 64 * j);
+            for (int j = 0; j < D / 64; ++j) a[i][j] = *(const v4i *)(from + 64 * j);
         }
     }
     // d / 16 channels, from d / 16 m on, of the lane's 16 keys
-    __device__ __forceinline__ void load_v(int step, int lane, uint32_t (&v)[16][D / 64]) const
+    __device__ __forceinline__ void load_v(const Place &p, int lane, uint32_t (&v)[16][D / 64]) const
     {
-        const int m = lane & 15, kb = lane >> 4;
-        Slot s = at(step * 64 + 16 * kb + (WHOLE ? 0 : m));
+        const bool is = there(p);
+        const int page = is ? p.entry : 0, at = is ? p.at : 0;
+        const int8_t *const from = c.v + head_v + (lane & 15) * (D / 16) + (WHOLE ? page * c.vs[0] + at * D : 0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            int page = max(s.page, 0), place = WHOLE ? s.at + i : s.at;
-            if constexpr (!WHOLE) {
-                page = __shfl(page, (lane & 48) + i);
-                place = __shfl(place, (lane & 48) + i);
-            }
-            const int8_t *at_ = c.v + head_v + page * c.vs[0] + place * c.vs[2] + m * (D / 16);
+            const int8_t *key = from + i * D;
+            if constexpr (!WHOLE) key = from + __shfl(page, (lane & 48) + i) * c.vs[0] + __shfl(at, (lane & 48) + i) * c.vs[2];
             if constexpr (D == 128) {
-                const uint2 w = *(const uint2 *)at_;
-                v[i][0] = w.x;
-                v[i][1] = w.y;
+                const v2i w = __builtin_nontemporal_load((const v2i *)key);
+                v[i][0] = (uint32_t)w[0];
+                v[i][1] = (uint32_t)w[1];
             } else {
-                v[i][0] = *(const uint32_t *)at_;
+                v[i][0] = __builtin_nontemporal_load((const uint32_t *)key);
             }
         }
     }
 };
+inline bool whole_pages(const CacheParams &c, int d) { return c.page_size % 16 == 0 && c.ks[2] == d && c.vs[2] == d; }
 
 // P.V of a step: acc[c] is channels d / 16 r + c of MFMA row r.  P_hat is unsigned and the MFMA signed: a byte of 128 or more
 // enters as P - 256, and where a wave holds one, 256 = 2 + 127 + 127 times V is added (kernel_common.h).
 template <int D> __device__ __forceinline__ void step_pv(const uint32_t (&v)[16][D / 64], const v4i pf, v4i (&acc)[D / 16])
 {
-    v4i t[D / 16];
+    const bool big = __any(((pf[0] | pf[1] | pf[2] | pf[3]) & (int)0x80808080u) != 0);
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+    for (int j = 0; j < D / 64; ++j) {
+        v4i t[4];
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
+        for (int g = 0; g < 4; ++g) {
             uint32_t o[4];
             transpose4(v[4 * g][j], v[4 * g + 1][j], v[4 * g + 2][j], v[4 * g + 3][j], o);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) t[4 * j + c][g] = (int)o[c];
+            for (int c = 0; c < 4; ++c) t[c][g] = (int)o[c];
         }
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], pf, acc[c], 0, 0, 0);
-    if (__any(((pf[0] | pf[1] | pf[2] | pf[3]) & (int)0x80808080u) != 0)) {
-        v4i two, big;
+        for (int c = 0; c < 4; ++c) acc[4 * j + c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], pf, acc[4 * j + c], 0, 0, 0);
+        if (big) {
+            v4i two, most;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            two[g] = (int)(((uint32_t)pf[g] >> 6) & 0x02020202u);
-            big[g] = (int)(((uint32_t)two[g] << 6) - ((uint32_t)two[g] >> 1)); // 127 in place of 2
-        }
+            for (int g = 0; g < 4; ++g) {
+                two[g] = (int)(((uint32_t)pf[g] >> 6) & 0x02020202u);
+                most[g] = (int)(((uint32_t)two[g] << 6) - ((uint32_t)two[g] >> 1)); // 127 in place of 2
+            }
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], two, acc[c], 0, 0, 0);
-            acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], big, acc[c], 0, 0, 0);
-            acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], big, acc[c], 0, 0, 0);
+            for (int c = 0; c < 4; ++c) {
+                acc[4 * j + c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], two, acc[4 * j + c], 0, 0, 0);
+                acc[4 * j + c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], most, acc[4 * j + c], 0, 0, 0);
+                acc[4 * j + c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t[c], most, acc[4 * j + c], 0, 0, 0);
+            }
         }
     }
 }
@@ -173,6 +182,7 @@ template <int D> __device__ __forceinline__ void load_q(const AttendParams &p, i
     }
 }
 
+// (left of lanes without a row: any, as long as it does not hold the others up)
 // scores of the lane's row for its 16 keys, sc[ii][i] that of key 16 kb + 4 ii + i; HIDDEN past the row's limit (left: what is left
 // of it at the lane's first key) and where the page is not there
 template <int D> __device__ __forceinline__ void step_scores(const v4i (&a)[4][D / 64], const bool (&there)[4], const v4i (&qf)[D / 64], int left, int kb, v4i (&sc)[4])
@@ -185,6 +195,7 @@ template <int D> __device__ __forceinline__ void step_scores(const v4i (&a)[4][D
 #pragma unroll
         for (int ii = 0; ii < 4; ++ii) sc[ii][i] = d[ii];
     }
+    if (__all(there[0] && there[1] && there[2] && there[3] && left >= 16)) return; // nearly all steps
     uint32_t seen[4]; // bit m: key 4 m + i is there
 #pragma unroll
     for (int i = 0; i < 4; ++i) seen[i] = ((uint32_t)__ballot(there[i]) & 0xffffu) >> (4 * kb);
@@ -195,14 +206,14 @@ template <int D> __device__ __forceinline__ void step_scores(const v4i (&a)[4][D
 }
 
 // the table index of four scores (bytes of the result), and the sum of their entries
-__device__ __forceinline__ uint32_t four_indices(const int4 x, int top, const RowParams &rp, const uint8_t *entry, int &sum)
+__device__ __forceinline__ uint32_t four_indices(const int4 x, int top, int c_int, double factor, const uint8_t *entry, int &sum)
 {
     const int sc[4] = {x.x, x.y, x.z, x.w};
     uint32_t word = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t away = min((uint32_t)top - (uint32_t)sc[i], (uint32_t)rp.c_int);
-        const uint32_t idx = (uint32_t)(int)__builtin_fma((double)(int)away, rp.factor, 0.5);
+        const uint32_t away = min((uint32_t)top - (uint32_t)sc[i], (uint32_t)c_int);
+        const uint32_t idx = (uint32_t)(int)__builtin_fma((double)(int)away, factor, 0.5);
         sum += entry[idx];
         word |= idx << (8 * i);
     }
@@ -215,28 +226,34 @@ __device__ __forceinline__ uint8_t *out_row(const AttendParams &p, int b, int kv
     return p.out + b * p.os[0] + (int64_t)(kvh * p.group + row / p.L) * p.os[1] + (row % p.L) * p.os[2];
 }
 
-// sums over the 16 lanes of a row of lanes: lane n ends with the sum of their x[n]
-__device__ __forceinline__ float scatter_sum16(float (&x)[16], int n)
+// Workgroup barrier that orders LDS accesses only: global loads requested before it stay in flight across it (__syncthreads() waits
+// for them).
+__device__ __forceinline__ void lds_barrier()
 {
-#pragma unroll
-    for (int h = 8; h >= 1; h /= 2) {
-        const bool up = (n & h) != 0;
-#pragma unroll
-        for (int j = 0; j < h; ++j) {
-            const float send = up ? x[j] : x[j + h], keep = up ? x[j + h] : x[j];
-            x[j] = keep + __shfl_xor(send, h);
-        }
-    }
-    return x[0];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-__device__ __forceinline__ void store_out(const AttendParams &p, const RowParams &rp, uint8_t *at, int ch, int acc)
+// What a step's key, one for each lane, has drawn from `rows` rows: idx holds the indices of row n's keys 16 kb .. + 15 at (n, kb),
+// 16 bytes each, so that a lane's bytes of all rows lie 64 apart.  The wave wrote them itself.
+__device__ __forceinline__ float drawn_by(const uint8_t *idx, const float (*share)[64], int rows, int lane)
+{
+    __builtin_amdgcn_wave_barrier();
+    float sum = 0.0f;
+    for (int r = 0; r < rows; ++r) sum += share[r][idx[64 * r + lane]];
+    __builtin_amdgcn_wave_barrier();
+    return sum;
+}
+
+// channel ch of an output row; mult and shift (INT8) or unit of the row's parameters
+__device__ __forceinline__ void store_out(const AttendParams &p, float unit, int mult, int shift, uint8_t *at, int ch, int acc)
 {
     if (p.out_type == 3) {
-        at[ch] = (uint8_t)(int8_t)requant_any(acc, rp.mult, rp.shift);
+        at[ch] = (uint8_t)(int8_t)requant_any(acc, mult, shift);
         return;
     }
-    const float x = (float)acc * rp.unit;
+    const float x = (float)acc * unit;
     if (p.out_type == 0) ((float *)at)[ch] = x;
     else if (p.out_type == 1) ((uint16_t *)at)[ch] = __builtin_bit_cast(uint16_t, (_Float16)x);
     else ((uint16_t *)at)[ch] = __builtin_bit_cast(uint16_t, (__bf16)x);

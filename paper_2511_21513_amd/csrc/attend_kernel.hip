@@ -1,39 +1,75 @@
 // Attention of the newest tokens over a paged INT8 cache (the pipeline of include/intattn.h, steps 1 to 8), for gfx950.
 //
 // IndexSoftmax needs the exact row maximum before any index and the exact row sum before any probability, so a row's keys are met
-// three times; K and V are read once each, because the scores, and then their table indices, stay in LDS (or, past its size, in
-// room of the context).  A workgroup takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens at a
-// time; its waves take every NW-th step of 64 keys and meet twice, at the maxima and at the sums.
+// three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  (What does not fit goes to
+// attend_split.hip.)  A workgroup takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens at a
+// time; its waves take every NW-th step of 64 keys and meet at the maxima and at the sums.
 #include "attend_common.h"
+
+#include <algorithm>
 
 namespace intattn {
 
 namespace {
 
-template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p)
+template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p)
 {
+    constexpr int BUF = PIPE ? 2 : 1;
+    using Place = typename Keys<D, WHOLE>::Place;
+    using PlaceK = typename Keys<D, WHOLE>::PlaceK;
     constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1; // (rows of accumulators a bank apart)
     __shared__ RowParams rowp[16];
-    __shared__ int wave_max[NW][16], wave_sum[NW][16], acc_sum[16 * ACC_ROW];
-    __shared__ uint8_t entry[64], prob[16][64]; // LUT_hat, and P_hat of each index in a row
+    __shared__ int row_max[16], row_sum[16], acc_sum[16 * ACC_ROW];
+    __shared__ uint8_t entry[64], prob[16][PROB]; // LUT_hat, and P_hat of each index in a row
     __shared__ float share[16][64];             // E / S
-    extern __shared__ int4 held[];              // scores of the first lds_steps steps
+    __shared__ int4 widx[NW][64];               // indices of a wave's step
+    extern __shared__ int4 held[];              // the sixteen scores, then indices, of each lane that has a row, step after step
 
     const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
     const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
-    const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1], len};
+    const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
     const int held_rows = min(p.rows, 16);
-    int4 *const spill = (int4 *)(p.scores + blockIdx.x * p.scores_wg);
-    // the lane's sixteen scores, then indices, of a step
-    auto place = [&](int s) {
-        const int at = (s * 4 + kb) * held_rows + n;
-        return s < p.lds_steps ? held + 4 * at : spill + 4 * (at - p.lds_steps * 4 * held_rows);
-    };
+    float *const weight_out = p.weight ? p.weight_out + b * p.wost[0] + kvh * p.wost[1] : nullptr;
+    auto place = [&](int s) { return held + 4 * ((s * 4 + kb) * held_rows + n); };
+    if (steps == 0) { // no keys: zeros
+        for (int i = threadIdx.x; i < p.rows * D; i += 64 * NW) store_out(p, 0.0f, 0, 31, out_row(p, b, kvh, i / D), i % D, 0);
+        return;
+    }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
 
     for (int blk = 0; blk < p.blocks; ++blk) {
         const int row = blk * 16 + n;
+        // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
+        // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
+        // them a wait could no longer count them
+        const float *const weight = !p.weight ? nullptr : blk == 0 ? p.weight + b * p.wst[0] + kvh * p.wst[1] : weight_out;
+        v4i a[BUF][4][KB], qf[KB];
+        bool there[BUF][4];
+        uint32_t v[BUF][16][KB];
+        float old[BUF];
+        auto ask_v = [&](int s, const Place &from, uint32_t (&vv)[16][KB], float &w) {
+            keys.load_v(from, lane, vv);
+            w = 0.0f;
+            if (weight) w = weight[min(s * 64 + lane, len - 1)]; // uniform
+        };
+        const int last = steps - 1;
+        Place pv[2];
+        PlaceK pk[2];
+        if constexpr (PIPE) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + i * NW, last), lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) keys.load_k(pk[i], lane, a[i], there[i]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + (2 + i) * NW, last), lane);
+        } else {
+            pk[0] = keys.find_k(wave, lane);
+            pv[0] = keys.find_v(wave, lane);
+            keys.load_k(pk[0], lane, a[0], there[0]);
+            ask_v(wave, pv[0], v[0], old[0]);
+        }
+        load_q<D>(p, b, kvh, row, kb, qf);
         if (threadIdx.x < 16) {
             RowParams rp = {1.0, 0.0f, 1, 0, 0, 31};
             if (row < p.rows) {
@@ -41,21 +77,19 @@ template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void 
                 if (row_params(p, b, kvh * p.group + row / p.L, t, kvh, rp) && t < fresh) rp.limit = len - fresh + t + 1;
             }
             rowp[n] = rp;
+            row_max[n] = HIDDEN;
+            row_sum[n] = 0;
         }
         for (int i = threadIdx.x; i < 16 * ACC_ROW; i += 64 * NW) acc_sum[i] = 0;
-        v4i qf[KB];
-        load_q<D>(p, b, kvh, row, kb, qf);
-        __syncthreads();
-        const RowParams rp = rowp[n];
+        lds_barrier();
         const bool mine = n < held_rows;
+        const int limit = mine ? rowp[n].limit : 0x7fffffff;
 
         // Q.K^T and row maxima
         int top = HIDDEN;
-        for (int s = wave; s < steps; s += NW) {
-            v4i a[4][KB], sc[4];
-            bool there[4];
-            keys.load_k(s, lane, a, there);
-            step_scores<D>(a, there, qf, rp.limit - (s * 64 + 16 * kb), kb, sc);
+        auto take_k = [&](int s, const v4i (&ka)[4][KB], const bool (&kt)[4]) {
+            v4i sc[4];
+            step_scores<D>(ka, kt, qf, limit - (s * 64 + 16 * kb), kb, sc);
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
             if (mine) {
@@ -63,123 +97,149 @@ template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void 
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii) at[ii] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
             }
+        };
+        if constexpr (PIPE) {
+            for (int s = wave; s < steps; s += 2 * NW) {
+                take_k(s, a[0], there[0]);
+                keys.load_k(pk[0], lane, a[0], there[0]);
+                pk[0] = keys.find_k(min(s + 4 * NW, last), lane);
+                if (s + NW < steps) take_k(s + NW, a[1], there[1]);
+                keys.load_k(pk[1], lane, a[1], there[1]);
+                pk[1] = keys.find_k(min(s + 5 * NW, last), lane);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + i * NW, last), lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) ask_v(min(wave + i * NW, last), pv[i], v[i], old[i]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + (2 + i) * NW, last), lane);
+        } else {
+            for (int s = wave; s < steps;) {
+                take_k(s, a[0], there[0]);
+                s += NW;
+                if (s < steps) keys.load_k(keys.find_k(s, lane), lane, a[0], there[0]);
+            }
         }
         top = max(top, __shfl_xor(top, 16));
         top = max(top, __shfl_xor(top, 32));
-        if (kb == 0) wave_max[wave][n] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < NW; ++w) top = max(top, wave_max[w][n]);
+        if (kb == 0 && mine) atomicMax(&row_max[n], top);
+        lds_barrier();
 
-        // indices and row sums
-        int sum = 0;
-        if (mine) {
-            for (int s = wave; s < steps; s += NW) {
-                int4 *at = place(s);
-                uint32_t word[4];
+        // indices and row sums: sixteen scores of a row to a thread, whichever wave they came from, so that all lanes have work
+        // (by the lanes that hold the rows it took 20 us of 115 at four rows and 8192 keys)
+        for (int i = threadIdx.x; i < steps * 4 * held_rows; i += 64 * NW) {
+            const int r = i % held_rows;
+            int4 *const at = held + 4 * i;
+            const int c_int = rowp[r].c_int, row_top = row_max[r];
+            const double factor = rowp[r].factor;
+            int sum = 0;
+            uint32_t word[4];
 #pragma unroll
-                for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(at[ii], top, rp, entry, sum);
-                at[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
-            }
+            for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(at[ii], row_top, c_int, factor, entry, sum);
+            at[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+            atomicAdd(&row_sum[r], sum);
         }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (kb == 0) wave_sum[wave][n] = sum;
-        __syncthreads();
+        lds_barrier();
         // tables of the rows: a wave fills row after row
-        for (int r = wave; r < 16; r += NW) {
-            int total = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) total += wave_sum[w][r];
-            const int row_top = __shfl(top, r);
-            const uint32_t e = lane <= p.top && row_top != HIDDEN ? entry[lane] : 0u, S = (uint32_t)max(total, 1);
+        for (int r = wave; r < held_rows; r += NW) {
+            const uint32_t e = lane <= p.top && row_max[r] != HIDDEN ? entry[lane] : 0u, S = (uint32_t)max(row_sum[r], 1);
             prob[r][lane] = (uint8_t)prob_u8(e, S, __builtin_amdgcn_rcpf((float)(2u * S)));
             share[r][lane] = (float)e / (float)S;
         }
-        __syncthreads();
+        lds_barrier();
 
         // P.V and the keys' weights
         v4i acc[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
-        for (int s = wave; s < steps; s += NW) {
-            uint32_t v[16][KB];
-            keys.load_v(s, lane, v);
+        auto take_v = [&](int s, const uint32_t (&vv)[16][KB], float before) {
             uint32_t word[4] = {0, 0, 0, 0};
             if (mine) {
                 const int4 x = *place(s);
                 word[0] = (uint32_t)x.x, word[1] = (uint32_t)x.y, word[2] = (uint32_t)x.z, word[3] = (uint32_t)x.w;
             }
             v4i pf = {0, 0, 0, 0};
-            float w[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const uint32_t idx = (word[j / 4] >> (8 * (j & 3))) & 0xffu;
-                const uint32_t pr = mine ? prob[n][idx] : 0u;
+                const uint32_t pr = prob[n][(word[j / 4] >> (8 * (j & 3))) & 0xffu];
                 pf[j / 4] |= (int)(pr << (8 * (j & 3)));
-                w[j] = 0.0f;
-                if (p.weight) w[j] = mine ? share[n][idx] : 0.0f;
             }
-            step_pv<D>(v, pf, acc);
-            if (p.weight) { // uniform
-                const float drawn = scatter_sum16(w, n);
-                const int slot = s * 64 + 16 * kb + n;
-                if (slot < len) {
-                    float *to = p.weight_out + b * p.wost[0] + kvh * p.wost[1] + slot;
-                    *to = blk == 0 ? p.decay * p.weight[b * p.wst[0] + kvh * p.wst[1] + slot] + drawn : *to + drawn;
-                }
+            if (!mine) pf = v4i{0, 0, 0, 0};
+            step_pv<D>(vv, pf, acc);
+            if (weight_out) { // uniform
+                if (mine) widx[wave][n * 4 + kb] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+                const float drawn = drawn_by((const uint8_t *)widx[wave], share, held_rows, lane);
+                const int slot = s * 64 + lane;
+                if (slot < len) weight_out[slot] = (blk == 0 ? p.decay * before : before) + drawn; // (further rows add to what the lane itself wrote)
+            }
+        };
+        if constexpr (PIPE) {
+            for (int s = wave; s < steps; s += 2 * NW) {
+                take_v(s, v[0], old[0]);
+                ask_v(min(s + 2 * NW, last), pv[0], v[0], old[0]);
+                pv[0] = keys.find_v(min(s + 4 * NW, last), lane);
+                if (s + NW < steps) take_v(s + NW, v[1], old[1]);
+                ask_v(min(s + 3 * NW, last), pv[1], v[1], old[1]);
+                pv[1] = keys.find_v(min(s + 5 * NW, last), lane);
+            }
+        } else {
+            for (int s = wave; s < steps;) {
+                take_v(s, v[0], old[0]);
+                s += NW;
+                if (s < steps) ask_v(s, keys.find_v(s, lane), v[0], old[0]);
             }
         }
-        if (mine) {
+        if (mine && wave < steps) {
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
         }
-        __syncthreads();
+        lds_barrier();
         for (int i = threadIdx.x; i < held_rows * D; i += 64 * NW) {
             const int r = i / D, ch = i % D, g = blk * 16 + r;
-            if (g < p.rows) store_out(p, rowp[r], out_row(p, b, kvh, g), ch, acc_sum[r * ACC_ROW + ch]);
+            if (g < p.rows) store_out(p, rowp[r].unit, rowp[r].mult, rowp[r].shift, out_row(p, b, kvh, g), ch, acc_sum[r * ACC_ROW + ch]);
         }
-        __syncthreads(); // before the next rows' parameters
+        lds_barrier(); // before the next rows' parameters
     }
 }
 
 } // namespace
 
-// LDS for the scores of a workgroup; the rest of its steps go to room of the context
-static constexpr int HELD_BYTES = 120 * 1024;
+// LDS for the scores of a workgroup
+static constexpr int HELD_BYTES = 128 * 1024;
 
-static int step_bytes(const AttendParams &p) { return 4 * 64 * (p.rows < 16 ? p.rows : 16); }
 static int most_steps(const AttendParams &p) { return (p.c.capacity + 63) / 64; }
-static int held_steps(const AttendParams &p)
+static int held_bytes(const AttendParams &p) { return most_steps(p) * 4 * 64 * (p.rows < 16 ? p.rows : 16); }
+
+// Whether the keys are split over workgroups: where the scores do not fit LDS, or where a model of both times, in us, says so.  One
+// launch takes 8 and a little for each step of the longest sequence in its workgroup, or for all bytes through the chip; three take 26
+// and what all bytes need (d 128, four rows a KV head, one launch against three with the gaps between them; 8 KV heads: 1 x 2048 keys 18.8 and
+// 24.5, 1 x 4096 36 and 26, 8 x 2048 24.7 and 29, 8 x 4096 40.4 and 34, 16 x 4096 42.5 and 46, 32 x 8192 104 and 139).
+static bool split_serves(const AttendParams &p, int d)
 {
-    const int fit = HELD_BYTES / step_bytes(p);
-    return fit < most_steps(p) ? fit : most_steps(p);
+    if (held_bytes(p) > HELD_BYTES) return true;
+    const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv, size = d / 128.0;
+    const double one = 8.0 + std::max(0.55 * steps * size, 0.0031 * all * size) * p.blocks, three = 26.0 + 0.0035 * all * size;
+    return three < one;
 }
 
-static bool split_serves(const AttendParams &p) { return p.c.capacity > 1024; }
-
-int64_t attend_room(const AttendParams &p, int d)
+template <int D, bool WHOLE> static void launch_waves(const AttendParams &p, void *stream)
 {
-    if (split_serves(p)) return attend_split_room(p, d, nullptr, nullptr);
-    return (int64_t)(most_steps(p) - held_steps(p)) * step_bytes(p) * p.c.B * p.c.Hkv;
+    const int waves = most_steps(p) <= 4 ? 4 : 8;
+    const bool pipe = most_steps(p) > 32; // two steps in flight: 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1
+    void (*kernel)(const AttendParams) = waves == 4 ? attend_kernel<D, 4, WHOLE, false> : pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv)), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p), (hipStream_t)stream, p);
 }
 
-int launch_attend(const AttendParams &p_, int d, void *room, void *stream)
+int64_t attend_room(const AttendParams &p, int d) { return split_serves(p, d) ? attend_split_room(p, d, nullptr, nullptr) : 0; }
+
+int launch_attend(const AttendParams &p, int d, void *room, void *stream)
 {
-    if (split_serves(p_)) return launch_attend_split(p_, d, room, stream);
-    AttendParams p = p_;
-    p.lds_steps = held_steps(p);
-    p.scores = (int32_t *)room;
-    p.scores_wg = (int64_t)(most_steps(p) - p.lds_steps) * step_bytes(p) / 4;
-    const bool whole = p.c.page_size % 16 == 0;
-    const size_t lds = (size_t)p.lds_steps * (size_t)step_bytes(p);
-    const bool few = most_steps(p) <= 4;
-    void (*kernel)(const AttendParams);
-    if (d == 64) kernel = few ? (whole ? attend_kernel<64, 4, true> : attend_kernel<64, 4, false>) : (whole ? attend_kernel<64, 8, true> : attend_kernel<64, 8, false>);
-    else kernel = few ? (whole ? attend_kernel<128, 4, true> : attend_kernel<128, 4, false>) : (whole ? attend_kernel<128, 8, true> : attend_kernel<128, 8, false>);
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv)), dim3(few ? 256 : 512), lds, (hipStream_t)stream, p);
+    if (split_serves(p, d)) return launch_attend_split(p, d, room, stream);
+    const bool whole = whole_pages(p.c, d);
+    if (d == 64) whole ? launch_waves<64, true>(p, stream) : launch_waves<64, false>(p, stream);
+    else whole ? launch_waves<128, true>(p, stream) : launch_waves<128, false>(p, stream);
     return (int)hipGetLastError();
 }
 

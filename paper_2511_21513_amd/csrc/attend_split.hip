@@ -11,6 +11,9 @@
 // indices of (row, kb) take the place of its first four scores.
 #include "attend_common.h"
 
+#include <algorithm>
+
+
 namespace intattn {
 
 namespace {
@@ -46,11 +49,19 @@ template <int D, bool WHOLE, bool ONE> __global__ __launch_bounds__(SNT) void ca
     __shared__ v4i q_lds[ONE ? 1 : SBLK][KB][64];
     const int chunk = blockIdx.x, g = blockIdx.y, blk0 = blockIdx.z * SBLK;
     const Group gr = group_of(p, g);
-    const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
+    const int s0 = chunk * p.score_steps, s1 = min(s0 + p.score_steps, gr.steps);
+    if (chunk == 0) {
+        for (int i = threadIdx.x; i < SROWS && blk0 * 16 + i < p.rows; i += SNT) { // for the other launches
+            const int row = blk0 * 16 + i;
+            RowParams rp;
+            rp.limit = row_params(p, gr.b, gr.kvh * p.group + row / p.L, row % p.L, gr.kvh, rp);
+            p.row_params[(int64_t)g * p.rows + row] = rp;
+        }
+    }
     if (s0 >= s1) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
     const int blocks = ONE ? 1 : min(SBLK, p.blocks - blk0);
-    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1], gr.len};
+    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1]};
     v4i qf[KB];
     if constexpr (ONE) {
         load_q<D>(p, gr.b, gr.kvh, n, kb, qf);
@@ -66,20 +77,22 @@ template <int D, bool WHOLE, bool ONE> __global__ __launch_bounds__(SNT) void ca
         most[i] = HIDDEN;
     }
     __syncthreads();
+    typename Keys<D, WHOLE>::PlaceK at = keys.find_k(s0 + wave, lane);
     for (int s = s0 + wave; s < s1; s += SWAVES) {
         v4i a[4][KB];
         bool there[4];
-        keys.load_k(s, lane, a, there);
+        keys.load_k(at, lane, a, there);
+        at = keys.find_k(s + SWAVES, lane);
         int4 *const to = step_of(p, g, s);
         for (int i = 0; i < blocks; ++i) {
             if constexpr (!ONE) {
 #pragma unroll
                 for (int j = 0; j < KB; ++j) qf[j] = q_lds[i][j][lane];
             }
-            v4i sc[4];
-            step_scores<D>(a, there, qf, limit[i * 16 + n] - (s * 64 + 16 * kb), kb, sc);
-            int top = HIDDEN;
             const int row = (blk0 + i) * 16 + n;
+            v4i sc[4];
+            step_scores<D>(a, there, qf, (row < p.rows ? limit[i * 16 + n] : 0x7fffffff) - (s * 64 + 16 * kb), kb, sc);
+            int top = HIDDEN;
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) {
                 top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
@@ -93,7 +106,7 @@ template <int D, bool WHOLE, bool ONE> __global__ __launch_bounds__(SNT) void ca
     __syncthreads();
     for (int i = threadIdx.x; i < blocks * 16; i += SNT) {
         const int row = blk0 * 16 + i;
-        if (row < p.rows) p.part_max[((int64_t)g * p.chunks + chunk) * p.rows + row] = most[i];
+        if (row < p.rows) p.part_max[((int64_t)g * p.score_chunks + chunk) * p.rows + row] = most[i];
     }
 }
 
@@ -104,53 +117,60 @@ __global__ __launch_bounds__(SNT) void cache_lookup_kernel(const AttendParams p)
     __shared__ uint8_t entry[64];
     const int chunk = blockIdx.x, g = blockIdx.y, row0 = blockIdx.z * SROWS, rows = min(SROWS, p.rows - row0);
     const Group gr = group_of(p, g);
-    const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
+    const int s0 = chunk * p.lookup_steps, s1 = min(s0 + p.lookup_steps, gr.steps);
     if (chunk == 0) // arrivals of the next launch
         for (int i = threadIdx.x; i < (rows + 15) / 16; i += SNT) p.arrived[g * p.blocks + row0 / 16 + i] = 0;
     if (s0 >= s1) return;
-    const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
+    const int per_step = rows * 4, items = (s1 - s0) * per_step, live = (gr.steps + p.score_steps - 1) / p.score_steps;
+    // the first scores are asked for before the row's maximum is known
+    auto at = [&](int i) {
+        const int s = i / per_step;
+        return step_of(p, g, s0 + s) + row0 * 4 + (i - s * per_step);
+    };
+    int4 x[4];
+    if ((int)threadIdx.x < items) {
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) x[ii] = at(threadIdx.x)[ii * p.rows * 4];
+    }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
     for (int i = threadIdx.x; i < rows; i += SNT) {
         most[i] = HIDDEN;
         total[i] = 0;
-        const int row = row0 + i;
-        RowParams rp;
-        const bool ok = row_params(p, gr.b, gr.kvh * p.group + row / p.L, row % p.L, gr.kvh, rp);
-        rp.limit = ok;
-        rowp[i] = rp;
+        rowp[i] = p.row_params[(int64_t)g * p.rows + row0 + i];
     }
-    __syncthreads();
+    lds_barrier();
     for (int i = threadIdx.x; i < rows * live; i += SNT)
-        atomicMax(&most[i % rows], p.part_max[((int64_t)g * p.chunks + i / rows) * p.rows + row0 + i % rows]);
-    __syncthreads();
-    const int per_step = rows * 4;
-    for (int i = threadIdx.x; i < (s1 - s0) * per_step; i += SNT) {
-        const int s = i / per_step, at = i % per_step, r = at / 4;
-        int4 *const from = step_of(p, g, s0 + s) + row0 * 4 + at;
-        int4 x[4];
+        atomicMax(&most[i % rows], p.part_max[((int64_t)g * p.score_chunks + i / rows) * p.rows + row0 + i % rows]);
+    lds_barrier();
+    for (int i = threadIdx.x; i < items; i += SNT) {
+        int4 *const from = at(i);
+        if (i >= SNT) {
 #pragma unroll
-        for (int ii = 0; ii < 4; ++ii) x[ii] = from[ii * p.rows * 4];
-        const RowParams rp = rowp[r];
-        const int top = most[r];
+            for (int ii = 0; ii < 4; ++ii) x[ii] = from[ii * p.rows * 4];
+        }
+        const int r = i % per_step / 4;
+        const int top = most[r], c_int = rowp[r].c_int;
+        const double factor = rowp[r].factor;
         int sum = 0;
         uint32_t word[4];
 #pragma unroll
-        for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(x[ii], top, rp, entry, sum);
+        for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(x[ii], top, c_int, factor, entry, sum);
         from[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
         atomicAdd(&total[r], sum);
     }
-    __syncthreads();
+    lds_barrier();
     for (int i = threadIdx.x; i < rows; i += SNT) // a row that sees nothing, or has no scale: 0
-        p.part_sum[((int64_t)g * p.chunks + chunk) * p.rows + row0 + i] = most[i] == HIDDEN || !rowp[i].limit ? 0 : total[i];
+        p.part_sum[((int64_t)g * p.lookup_chunks + chunk) * p.rows + row0 + i] = most[i] == HIDDEN || !rowp[i].limit ? 0 : total[i];
 }
 
 // P_hat and E / S of each index for 16 rows from row0 on; S = 0: zeros
-__device__ __forceinline__ void row_tables(const AttendParams &p, int g, int row0, int live, uint8_t (*prob)[64], float (*share)[64])
+__device__ __forceinline__ void row_tables(const AttendParams &p, int g, int steps, int row0, uint8_t (*prob)[PROB], float (*share)[64])
 {
+    const int live = (steps + p.lookup_steps - 1) / p.lookup_steps;
     const int r = threadIdx.x >> 4, part = threadIdx.x & 15, row = row0 + r;
     int sum = 0;
     if (row < p.rows)
-        for (int c = part; c < live; c += 16) sum += p.part_sum[((int64_t)g * p.chunks + c) * p.rows + row];
+        for (int c = part; c < live; c += 16) sum += p.part_sum[((int64_t)g * p.lookup_chunks + c) * p.rows + row];
 #pragma unroll
     for (int o = 1; o < 16; o *= 2) sum += __shfl_xor(sum, o);
     const uint32_t S = (uint32_t)max(sum, 1);
@@ -167,8 +187,9 @@ __device__ __forceinline__ void row_tables(const AttendParams &p, int g, int row
 template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void cache_values_kernel(const AttendParams p)
 {
     constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1;
-    __shared__ uint8_t prob[16][64];
+    __shared__ uint8_t prob[16][PROB];
     __shared__ float share[WEIGHT ? 16 : 1][64];
+    __shared__ int4 widx[WEIGHT ? SWAVES : 1][64];
     __shared__ int acc_sum[16 * ACC_ROW];
     __shared__ int last;
     const int chunk = blockIdx.x, g = blockIdx.y, blk = blockIdx.z;
@@ -176,38 +197,66 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
     const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
     if (chunk > 0 && s0 >= s1) return;
     const int live = max((gr.steps + p.chunk_steps - 1) / p.chunk_steps, 1);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4, row = blk * 16 + n;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4, row = blk * 16 + n;
     const int rows = min(16, p.rows - blk * 16);
-    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1], gr.len};
-    row_tables(p, g, blk * 16, gr.steps > 0 ? live : 0, prob, WEIGHT ? share : nullptr);
-    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += SNT) acc_sum[i] = 0;
-    __syncthreads();
+    const Keys<D, WHOLE> keys{p.c, p.c.table + gr.b * p.c.table_stride, gr.kvh * p.c.ks[1], gr.kvh * p.c.vs[1]};
     const bool mine = n < rows;
+    const float *const weight = WEIGHT ? p.weight + gr.b * p.wst[0] + gr.kvh * p.wst[1] : nullptr;
+    float *const weight_out = WEIGHT ? p.weight_out + gr.b * p.wost[0] + gr.kvh * p.wost[1] : nullptr;
+
+    // what a step reads, requested for two steps at a time
+    struct Step {
+        uint32_t v[16][KB];
+        int4 x;
+        float old;
+    } st[2];
+    typename Keys<D, WHOLE>::Place at[2];
+    auto request = [&](int s, int i) {
+        Step &to = st[i];
+        keys.load_v(at[i], lane, to.v);
+        to.x = step_of(p, g, s)[(mine ? row : blk * 16) * 4 + kb];
+        if constexpr (WEIGHT) to.old = weight[min(s * 64 + lane, gr.len - 1)];
+    };
+    const int first = s0 + wave;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + i * SWAVES, lane);
+    if (first < s1) {
+        request(first, 0);
+        if (first + SWAVES < s1) request(first + SWAVES, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + (2 + i) * SWAVES, lane);
+    row_tables(p, g, gr.steps, blk * 16, prob, WEIGHT ? share : nullptr);
+    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += SNT) acc_sum[i] = 0;
+    lds_barrier();
     v4i acc[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
-    for (int s = s0 + wave; s < s1; s += SWAVES) {
-        uint32_t v[16][KB];
-        keys.load_v(s, lane, v);
-        int4 x = make_int4(0, 0, 0, 0);
-        if (mine) x = step_of(p, g, s)[row * 4 + kb];
-        const uint32_t word[4] = {(uint32_t)x.x, (uint32_t)x.y, (uint32_t)x.z, (uint32_t)x.w};
+    auto take = [&](int s, const Step &of) {
+        const uint32_t word[4] = {(uint32_t)of.x.x, (uint32_t)of.x.y, (uint32_t)of.x.z, (uint32_t)of.x.w};
         v4i pf = {0, 0, 0, 0};
-        float w[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const uint32_t idx = (word[j / 4] >> (8 * (j & 3))) & 0xffu;
-            const uint32_t pr = mine ? prob[n][idx] : 0u;
+            const uint32_t pr = prob[n][(word[j / 4] >> (8 * (j & 3))) & 0xffu];
             pf[j / 4] |= (int)(pr << (8 * (j & 3)));
-            if constexpr (WEIGHT) w[j] = mine ? share[n][idx] : 0.0f;
         }
-        step_pv<D>(v, pf, acc);
+        if (!mine) pf = v4i{0, 0, 0, 0};
+        step_pv<D>(of.v, pf, acc);
         if constexpr (WEIGHT) {
-            const float drawn = scatter_sum16(w, n);
-            const int slot = s * 64 + 16 * kb + n;
-            if (slot < gr.len)
-                p.weight_out[gr.b * p.wost[0] + gr.kvh * p.wost[1] + slot] = p.decay * p.weight[gr.b * p.wst[0] + gr.kvh * p.wst[1] + slot] + drawn;
+            if (mine) widx[wave][n * 4 + kb] = of.x;
+            const float drawn = drawn_by((const uint8_t *)widx[wave], share, rows, lane);
+            if (s * 64 + lane < gr.len) weight_out[s * 64 + lane] = p.decay * of.old + drawn;
         }
+    };
+    for (int s = first; s < s1; s += 2 * SWAVES) {
+        if (s != first) {
+            request(s, 0);
+            if (s + SWAVES < s1) request(s + SWAVES, 1);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) at[i] = keys.find_v(s + (2 + i) * SWAVES, lane);
+        }
+        take(s, st[0]);
+        if (s + SWAVES < s1) take(s + SWAVES, st[1]);
     }
     if (mine) {
 #pragma unroll
@@ -216,46 +265,58 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
             for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
     }
     __syncthreads();
-    int32_t *const part = p.part_acc + ((int64_t)g * p.blocks + blk) * p.chunks * 16 * D;
+    uint64_t *const part = (uint64_t *)(p.part_acc + ((int64_t)g * p.blocks + blk) * p.chunks * 16 * D);
+    constexpr int PART = 16 * D / 2; // pairs of accumulators of a chunk
     if (live > 1) {
         // device-scope stores and loads for what another workgroup reads: they pass the L2 of the XCD
-        for (int i = threadIdx.x; i < rows * D; i += SNT)
-            __hip_atomic_store(part + (int64_t)chunk * 16 * D + i, acc_sum[i / D * ACC_ROW + i % D], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int i = threadIdx.x; i < rows * D / 2; i += SNT) {
+            const int *a = &acc_sum[2 * i / D * ACC_ROW + 2 * i % D];
+            __hip_atomic_store(part + (int64_t)chunk * PART + i, (uint64_t)(uint32_t)a[0] | ((uint64_t)(uint32_t)a[1] << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) last = (int)atomicAdd((unsigned *)&p.arrived[g * p.blocks + blk], 1u);
         __syncthreads();
         if (last != live - 1) return;
     }
-    for (int i = threadIdx.x; i < rows * D; i += SNT) {
-        const int r = i / D, ch = i % D, out = blk * 16 + r;
-        int sum = 0;
+    for (int i = threadIdx.x; i < rows * D / 2; i += SNT) {
+        const int r = 2 * i / D, ch = 2 * i % D, out = blk * 16 + r;
+        int sum[2] = {acc_sum[r * ACC_ROW + ch], acc_sum[r * ACC_ROW + ch + 1]};
         if (live > 1) {
-            for (int c = 0; c < live; ++c) sum += __hip_atomic_load(part + (int64_t)c * 16 * D + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        } else {
-            sum = acc_sum[r * ACC_ROW + ch];
+            sum[0] = sum[1] = 0;
+            constexpr int BATCH = 32; // loads in flight
+            for (int c = 0; c < live; c += BATCH) {
+                uint64_t x[BATCH];
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) x[u] = __hip_atomic_load(part + (int64_t)min(c + u, live - 1) * PART + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    sum[0] += c + u < live ? (int)(uint32_t)x[u] : 0;
+                    sum[1] += c + u < live ? (int)(uint32_t)(x[u] >> 32) : 0;
+                }
+            }
         }
-        RowParams rp;
-        if (!row_params(p, gr.b, gr.kvh * p.group + out / p.L, out % p.L, gr.kvh, rp)) sum = 0;
-        store_out(p, rp, out_row(p, gr.b, gr.kvh, out), ch, sum);
+        const RowParams ro = p.row_params[(int64_t)g * p.rows + out];
+        uint8_t *const at = out_row(p, gr.b, gr.kvh, out);
+        store_out(p, ro.unit, ro.mult, ro.shift, at, ch, sum[0]);
+        store_out(p, ro.unit, ro.mult, ro.shift, at, ch + 1, sum[1]);
     }
 }
 
 // Weights where a KV head has more than 16 rows: a thread for each key, over all rows.
 __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p)
 {
-    __shared__ uint8_t prob[16][64];
+    __shared__ uint8_t prob[16][PROB];
     __shared__ float share[16][64];
     const int g = blockIdx.y;
     const Group gr = group_of(p, g);
     const int slot = blockIdx.x * SNT + threadIdx.x;
     if ((int)blockIdx.x * SNT >= gr.len) return;
-    const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
     const bool mine = slot < gr.len;
     float drawn = 0.0f;
     for (int blk = 0; blk < p.blocks; ++blk) {
         __syncthreads();
-        row_tables(p, g, blk * 16, live, prob, share);
+        row_tables(p, g, gr.steps, blk * 16, prob, share);
         __syncthreads();
         const int rows = min(16, p.rows - blk * 16);
         if (mine) {
@@ -268,13 +329,23 @@ __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p
 
 } // namespace
 
+// Steps of a workgroup in each launch, by the number of steps there can be (one row, 32 sequences of 4000 to 12400 keys, and one of
+// 30011, d 128, us): scores, short workgroups, 4: 59.0, 9.1; 16: 69.5, 11.0.  Lookup, 8: 12.9, 4.6; 32: 10.2, 5.3.  Values, where
+// each workgroup leaves accumulators to be joined, 4: 128, 31.8; 8: 87, 21.2; 16: 73.3, 17.6; 32: 74.4, 22.1.
 static void plan(AttendParams &p)
 {
     p.steps = (p.c.capacity + 63) / 64;
     const int64_t all = (int64_t)p.steps * p.c.B * p.c.Hkv;
-    int64_t c = (all + 4095) / 4096;          // about 4096 workgroups, of a step for each wave at least
-    if (c < (p.steps + 63) / 64) c = (p.steps + 63) / 64; // and at most 64 chunks of a sequence
-    p.chunk_steps = (int32_t)((c + SWAVES - 1) / SWAVES * SWAVES);
+    // as many steps as leave `workgroups` workgroups, between `least` and what makes `most` chunks of a sequence
+    auto steps_of = [&](int64_t workgroups, int64_t least, int64_t most) {
+        const int64_t c = std::max(std::max((all + workgroups - 1) / workgroups, least), (p.steps + most - 1) / most);
+        return (int32_t)((c + SWAVES - 1) / SWAVES * SWAVES);
+    };
+    p.score_steps = steps_of(16384, 4, 256);
+    p.lookup_steps = steps_of(1536, 8, 256);
+    p.chunk_steps = steps_of(3072, 8, 32);
+    p.score_chunks = (p.steps + p.score_steps - 1) / p.score_steps;
+    p.lookup_chunks = (p.steps + p.lookup_steps - 1) / p.lookup_steps;
     p.chunks = (p.steps + p.chunk_steps - 1) / p.chunk_steps;
 }
 
@@ -290,10 +361,11 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
         return m;
     };
     p.scores = take(groups * p.steps * 64 * p.rows);
-    p.part_max = take(groups * p.chunks * p.rows);
-    p.part_sum = take(groups * p.chunks * p.rows);
+    p.part_max = take(groups * p.score_chunks * p.rows);
+    p.part_sum = take(groups * p.lookup_chunks * p.rows);
     p.part_acc = take(groups * p.blocks * p.chunks * 16 * d);
     p.arrived = take(groups * p.blocks);
+    p.row_params = (RowParams *)take(groups * p.rows * (int64_t)(sizeof(RowParams) / 4));
     if (out) *out = p;
     return 4 * at;
 }
@@ -301,9 +373,9 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
 template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, hipStream_t st)
 {
     const uint32_t groups = (uint32_t)(p.c.B * p.c.Hkv), supers = (uint32_t)((p.rows + SROWS - 1) / SROWS);
-    if (p.blocks == 1) hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, true>), dim3((uint32_t)p.chunks, groups, 1), dim3(SNT), 0, st, p);
-    else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.chunks, groups, supers), dim3(SNT), 0, st, p);
-    hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.chunks, groups, supers), dim3(SNT), 0, st, p);
+    if (p.blocks == 1) hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, true>), dim3((uint32_t)p.score_chunks, groups, 1), dim3(SNT), 0, st, p);
+    else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.score_chunks, groups, supers), dim3(SNT), 0, st, p);
+    hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.lookup_chunks, groups, supers), dim3(SNT), 0, st, p);
     const bool inside = p.weight && p.blocks == 1;
     hipLaunchKernelGGL((inside ? cache_values_kernel<D, WHOLE, true> : cache_values_kernel<D, WHOLE, false>), dim3((uint32_t)p.chunks, groups, (uint32_t)p.blocks),
                        dim3(SNT), 0, st, p);
@@ -314,7 +386,7 @@ int launch_attend_split(const AttendParams &p_, int d, void *room, void *stream)
 {
     AttendParams p;
     attend_split_room(p_, d, room, &p);
-    const bool whole = p.c.page_size % 16 == 0;
+    const bool whole = whole_pages(p.c, d);
     hipStream_t st = (hipStream_t)stream;
     if (d == 64) whole ? launch_split_d<64, true>(p, st) : launch_split_d<64, false>(p, st);
     else whole ? launch_split_d<128, true>(p, st) : launch_split_d<128, false>(p, st);

@@ -54,6 +54,15 @@ struct AppendParams {
     RotaryParams r;
 };
 
+// What the kernels need of a row of a KV head
+struct RowParams {
+    double factor;   // the double after top / c_int
+    float unit;      // floating-point output of one step of the accumulator
+    int32_t c_int;
+    int32_t limit;   // slots that the row sees (attend_split.hip: whether its scales are usable)
+    int32_t mult, shift;
+};
+
 struct AttendParams {
     CacheParams c;
     const int8_t *q;
@@ -74,14 +83,13 @@ struct AttendParams {
     int32_t top;
     double clip, sqrt_d;
     uint32_t lut[16];
-    int32_t *scores;           // room for scores that do not fit LDS: scores_step words for each step of 64 keys of a workgroup
-    int64_t scores_wg;         // words of a workgroup
-    int32_t lds_steps;         // steps of 64 keys whose scores LDS holds
-    // keys split over workgroups (attend_split.hip): chunks of chunk_steps steps, `chunks` of them and `steps` steps where a
-    // sequence has capacity slots.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks][rows], accumulators
-    // [group][block of rows][chunks][16][d], arrivals [group][block of rows]; a group is a (sequence, KV head)
-    int32_t steps, chunks, chunk_steps;
-    int32_t *part_max, *part_sum, *part_acc, *arrived;
+    // keys split over workgroups (attend_split.hip): steps of a sequence of capacity slots, and for each launch the steps of a
+    // workgroup and the workgroups of a sequence.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks of that
+    // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], parameters [group][rows]; a
+    // group is a (sequence, KV head)
+    int32_t steps, score_steps, score_chunks, lookup_steps, lookup_chunks, chunk_steps, chunks;
+    int32_t *scores, *part_max, *part_sum, *part_acc, *arrived;
+    RowParams *row_params;
 };
 
 struct EvictParams {
