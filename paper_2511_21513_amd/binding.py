@@ -158,6 +158,16 @@ class EvictArgs(ctypes.Structure):
     ]
 
 
+# the argument structs as one pack each, with the padding of the platform (an assignment for each field took most of a call's time)
+_ROTARY = "4iP3qP128s"
+_ROPE = struct.Struct("@4i2i2P2P6q6q" + _ROTARY)
+_APPEND = struct.Struct("@4i3P9qPP3qP" + _ROTARY + "3P4q")
+_CACHE_FORWARD = struct.Struct("@4iP3qPPP3qPPP4qfi")
+_EVICT = struct.Struct("@4i4P8q2P")
+for _s, _c in ((_ROPE, RopeArgs), (_APPEND, AppendArgs), (_CACHE_FORWARD, CacheForwardArgs), (_EVICT, EvictArgs)):
+    assert _s.size == ctypes.sizeof(_c)
+_NO_ROTATION = (0, 0, 0, 0, 0, 0, 0, 0, 0, b"")
+
 _lib = None
 _F32 = np.dtype(np.float32)
 
@@ -189,11 +199,11 @@ def load() -> ctypes.CDLL:
         lib.intattn_dynamic_status.restype = ctypes.c_int
         lib.intattn_index_softmax.argtypes = [vp, ctypes.POINTER(SoftmaxArgs), vp]
         lib.intattn_index_softmax.restype = ctypes.c_int
-        cache = ctypes.POINTER(Cache)
-        lib.intattn_rope.argtypes = [vp, ctypes.POINTER(RopeArgs), vp]
-        lib.intattn_cache_append.argtypes = [vp, cache, ctypes.POINTER(AppendArgs), vp]
-        lib.intattn_cache_forward.argtypes = [vp, cache, ctypes.POINTER(CacheForwardArgs), vp]
-        lib.intattn_cache_evict.argtypes = [vp, cache, ctypes.POINTER(EvictArgs), vp]
+        cache = ctypes.POINTER(Cache)  # (the other structs come packed, as bytes)
+        lib.intattn_rope.argtypes = [vp, vp, vp]
+        lib.intattn_cache_append.argtypes = [vp, cache, vp, vp]
+        lib.intattn_cache_forward.argtypes = [vp, cache, vp, vp]
+        lib.intattn_cache_evict.argtypes = [vp, cache, vp, vp]
         lib.intattn_cache_reserve.argtypes = [vp, cache, i32, i32, i32]
         for f in (lib.intattn_rope, lib.intattn_cache_append, lib.intattn_cache_forward, lib.intattn_cache_evict, lib.intattn_cache_reserve):
             f.restype = i32
@@ -243,28 +253,61 @@ def _ptr(t):
     return t.data_ptr() if t is not None else 0
 
 
-def _check(t, what, dtype, shape, device, contiguous=False):
-    """A tensor (or None) that the struct will point at: its type, shape and place, which pointers do not carry."""
-    if t is None:
-        return
-    if t.dtype != dtype or t.device != device or len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
+_types = {}
 
 
 def _float_types():
-    import torch
+    if not _types:
+        import torch
 
-    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        _types.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return _types
+
+
+def _check(t, what, dtype, shape, device, contiguous=False):
+    """A tensor (or None) that a struct will point at: its type, shape and device index, which pointers do not carry."""
+    if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != device or (contiguous and not t.is_contiguous())):
+        raise ValueError(f"{what} must be a {'contiguous ' if contiguous else ''}{dtype} tensor of shape {tuple(shape)} on cuda:{device}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _rows(t, what, dtype, shape, device):
+    """The same for [B, H, L, d] tensors whose last axis has to be contiguous: their strides."""
+    _check(t, what, dtype, shape, device)
+    st = t.stride()
+    if st[3] != 1:
+        raise ValueError(f"{what}: the head dimension must be contiguous")
+    return st
 
 
 def _slots(t, what, dtype, B, Hkv, slots, device):
-    """[B, Hkv, slots] planes: the last axis is contiguous and holds every slot the call may touch."""
-    _check(t, what, dtype, (B, Hkv, None), device)
-    if t is not None and (t.stride(2) != 1 or t.shape[2] < slots):
-        raise ValueError(f"{what} must hold {slots} slots, contiguous")
-    return t.stride()[:2] if t is not None else (0, 0)
+    """[B, Hkv, slots] planes (or None): the last axis is contiguous and holds every slot the call may touch."""
+    if t is None:
+        return 0, 0
+    if t.dim() != 3 or t.shape[2] < slots or t.stride(2) != 1:
+        raise ValueError(f"{what} must be [B, Hkv, slots] with at least {slots} slots, contiguous")
+    _check(t, what, dtype, (B, Hkv, t.shape[2]), device)
+    return t.stride()[:2]
+
+
+def _rotation(B, L, device, pos, freq, axis, pairing, inverse):
+    """The fields of intattn_rotary."""
+    import torch
+
+    if pos.dim() == 2:
+        pos = pos[None]
+    _check(pos, "pos", torch.int32, (pos.shape[0], B, L), device)
+    n = freq.shape[0]
+    _check(freq, "freq", torch.float64, (n,), device, True)
+    if n > 128:
+        raise ValueError("at most 128 rotated pairs")
+    if pairing not in ("adjacent", "halves"):
+        raise ValueError("pairing is 'adjacent' or 'halves'")
+    if axis is not None:
+        axis = bytes(axis)  # (raises unless each is 0 .. 255; the library compares them with the axes)
+        if len(axis) != n:
+            raise ValueError("axis must name an axis for each pair")
+    return (2 * n, int(pairing == "halves"), pos.shape[0], int(bool(inverse)), pos.data_ptr(), *pos.stride(), freq.data_ptr(), axis or b"")
 
 
 class PagedCache:
@@ -277,18 +320,15 @@ class PagedCache:
     def __init__(self, k_pages, v_pages, table, lens, scale_k, scale_v):
         import torch
 
-        dev = k_pages.device
-        if k_pages.dim() != 4 or not k_pages.is_cuda:
-            raise ValueError("k_pages must be an int8 tensor [n_pages, Hkv, page_size, d] on the GPU")
+        if k_pages.dim() != 4 or not k_pages.is_cuda or table.dim() != 2:
+            raise ValueError("k_pages must be an int8 tensor [n_pages, Hkv, page_size, d] on the GPU, table [B, max_pages]")
+        dev = k_pages.get_device()
         n_pages, Hkv, page, d = k_pages.shape
-        for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-            _check(t, what, torch.int8, (n_pages, Hkv, page, d), dev)
-            if t.stride(3) != 1:
-                raise ValueError("the head dimension must be contiguous")
-        _check(table, "table", torch.int32, (None, None), dev)
+        k_st, v_st = (_rows(t, what, torch.int8, (n_pages, Hkv, page, d), dev) for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")))
+        B = table.shape[0]
+        _check(table, "table", torch.int32, (B, table.shape[1]), dev)
         if table.shape[1] > 1 and table.stride(1) != 1:
             raise ValueError("rows of the table must be contiguous")
-        B = table.shape[0]
         _check(lens, "lens", torch.int32, (B,), dev, True)
         for t, what in ((scale_k, "scale_k"), (scale_v, "scale_v")):
             _check(t, what, torch.float32, (scale_k.numel(),), dev, True)
@@ -302,9 +342,10 @@ class PagedCache:
         c.scale_mode = int(scale_k.numel() == Hkv)
         c.k, c.v, c.table, c.lens = k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lens.data_ptr()
         c.scale_k, c.scale_v = scale_k.data_ptr(), scale_v.data_ptr()
-        c.k_stride[:], c.v_stride[:] = k_pages.stride()[:3], v_pages.stride()[:3]
+        c.k_stride[:], c.v_stride[:] = k_st[:3], v_st[:3]
         c.table_stride = table.stride(0)
         self.args = c
+        self._ref = ctypes.byref(c)
 
 
 class IntAttn:
@@ -555,30 +596,13 @@ class IntAttn:
     def _stream(self, device, stream):
         import torch
 
-        if device.index != self.device:
-            raise ValueError(f"tensors on {device}, context on device {self.device}")
-        return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream
+        if device != self.device:
+            raise ValueError(f"tensors on device {device}, context on device {self.device}")
+        return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream
 
-    @staticmethod
-    def _rotary(r, B, L, device, pos, freq, axis, pairing, inverse=False):
-        import torch
-
-        if pos.dim() == 2:
-            pos = pos[None]
-        _check(pos, "pos", torch.int32, (None, B, L), device)
-        _check(freq, "freq", torch.float64, (None,), device, True)
-        n = freq.shape[0]
-        if n > 128:
-            raise ValueError("at most 128 rotated pairs")
-        if pairing not in ("adjacent", "halves"):
-            raise ValueError("pairing is 'adjacent' or 'halves'")
-        r.rot, r.pairing, r.n_axes, r.inverse = 2 * n, int(pairing == "halves"), pos.shape[0], int(bool(inverse))
-        r.pos, r.freq = pos.data_ptr(), freq.data_ptr()
-        r.pos_stride[:] = pos.stride()
-        if axis is not None:
-            if len(axis) != n or min(axis) < 0 or max(axis) > 255:
-                raise ValueError("axis must name an axis for each pair")
-            r.axis[:n] = axis
+    def _done(self, rc):
+        if rc != OK:
+            raise IntAttnError(rc, self.last_error())
 
     def rope(self, x, pos, freq, *, axis=None, pairing="adjacent", inverse=False, out=None, stream=None):
         """intattn_rope on a [B, H, L, d] tensor, or on two with the same B, L, d (Q and K): new tensors, or ``out``, which may be
@@ -587,29 +611,24 @@ class IntAttn:
         import torch
 
         one = torch.is_tensor(x)
-        xs = [x] if one else list(x)
-        if not 1 <= len(xs) <= 2:
-            raise ValueError("one tensor or two")
+        xs = (x,) if one else x
         outs = [torch.empty_like(t) for t in xs] if out is None else [out] if torch.is_tensor(out) else list(out)
-        B, _, L, d = xs[0].shape
-        types, dev = _float_types(), xs[0].device
-        if xs[0].dtype not in types or len(outs) != len(xs):
-            raise ValueError("expected float32/float16/bfloat16 tensors and as many outputs")
-        a = RopeArgs()
-        a.B, a.L, a.d, a.dtype = B, L, d, types[xs[0].dtype]
-        es = xs[0].element_size()
-        for i, (t, o) in enumerate(zip(xs, outs)):
-            _check(t, "x", xs[0].dtype, (B, None, L, d), dev)
-            _check(o, "out", t.dtype, tuple(t.shape), dev)
-            if t.stride(3) != 1 or o.stride(3) != 1:
-                raise ValueError("the head dimension must be contiguous")
-            a.H[i], a.src[i], a.dst[i] = t.shape[1], t.data_ptr(), o.data_ptr()
-            for j in range(3):
-                a.src_stride[i][j], a.dst_stride[i][j] = t.stride(j) * es, o.stride(j) * es
-        self._rotary(a.rotary, B, L, dev, pos, freq, axis, pairing, inverse)
-        rc = self._lib.intattn_rope(self._ctx, ctypes.byref(a), ctypes.c_void_p(self._stream(dev, stream)))
-        if rc != OK:
-            raise IntAttnError(rc, self.last_error())
+        if not 1 <= len(xs) <= 2 or len(outs) != len(xs):
+            raise ValueError("one tensor or two, and as many outputs")
+        a, b = xs[0], xs[-1]
+        B, H, L, d = a.shape
+        dtype, dev, es, H2 = a.dtype, a.get_device(), a.element_size(), b.shape[1]
+        code = _float_types().get(dtype)
+        if code is None:
+            raise ValueError("expected float32/float16/bfloat16 tensors")
+        s0, s1, s2, _ = _rows(a, "x", dtype, a.shape, dev)
+        t0, t1, t2, _ = _rows(b, "x", dtype, (B, H2, L, d), dev)
+        o0, o1, o2, _ = _rows(outs[0], "out", dtype, a.shape, dev)
+        p0, p1, p2, _ = _rows(outs[-1], "out", dtype, b.shape, dev)
+        args = _ROPE.pack(B, L, d, code, H, 0 if len(xs) == 1 else H2, a.data_ptr(), b.data_ptr(), outs[0].data_ptr(), outs[-1].data_ptr(),
+                          s0 * es, s1 * es, s2 * es, t0 * es, t1 * es, t2 * es, o0 * es, o1 * es, o2 * es, p0 * es, p1 * es, p2 * es,
+                          *_rotation(B, L, dev, pos, freq, axis, pairing, inverse))
+        self._done(self._lib.intattn_rope(self._ctx, args, self._stream(dev, stream)))
         return outs[0] if one else outs
 
     def cache_append(self, cache: PagedCache, k, v, q=None, *, n_new=None, pos=None, freq=None, axis=None, pairing="adjacent",
@@ -619,78 +638,34 @@ class IntAttn:
         [B, Hq, L]."""
         import torch
 
-        types, dev, B, L = _float_types(), cache.device, cache.B, k.shape[2]
-        if k.dtype not in types:
+        dev, B, L, d, dtype = cache.device, cache.B, k.shape[2], cache.d, k.dtype
+        code = _float_types().get(dtype)
+        if code is None:
             raise ValueError("expected float32/float16/bfloat16 tensors")
-        Hq = q.shape[1] if q is not None else 0
-        es = k.element_size()
-        a = AppendArgs()
-        a.L, a.Hq, a.dtype = L, Hq, types[k.dtype]
-        for t, what, h, at in ((q, "q", Hq, a.q_stride), (k, "k", cache.Hkv, a.k_stride), (v, "v", cache.Hkv, a.v_stride)):
-            if t is None:
-                continue
-            _check(t, what, k.dtype, (B, h, L, cache.d), dev)
-            st = t.stride()
-            if st[3] != 1:
-                raise ValueError("the head dimension must be contiguous")
-            at[0], at[1], at[2] = st[0] * es, st[1] * es, st[2] * es
-        a.k, a.v, a.q = k.data_ptr(), v.data_ptr(), _ptr(q)
+        es, shape = k.element_size(), (B, cache.Hkv, L, d)
+        k0, k1, k2, _ = _rows(k, "k", dtype, shape, dev)
+        v0, v1, v2, _ = _rows(v, "v", dtype, shape, dev)
         _check(n_new, "n_new", torch.int32, (B,), dev, True)
-        a.n_new = _ptr(n_new)
+        Hq = q0 = q1 = q2 = o0 = o1 = o2 = 0
         if q is not None:
+            Hq = q.shape[1]
+            q0, q1, q2, _ = _rows(q, "q", dtype, (B, Hq, L, d), dev)
             if q_out is None:
-                q_out = torch.empty((B, Hq, L, cache.d), dtype=torch.int8, device=dev)
+                q_out = torch.empty((B, Hq, L, d), dtype=torch.int8, device=q.device)
             if q_scale is None:
-                q_scale = torch.empty((B, Hq, L), dtype=torch.float32, device=dev)
-            _check(q_out, "q_out", torch.int8, (B, Hq, L, cache.d), dev)
+                q_scale = torch.empty((B, Hq, L), dtype=torch.float32, device=q.device)
+            o0, o1, o2, _ = _rows(q_out, "q_out", torch.int8, (B, Hq, L, d), dev)
             _check(q_scale, "q_scale", torch.float32, (B, Hq, L), dev, True)
-            st = q_out.stride()
-            if st[3] != 1:
-                raise ValueError("the head dimension must be contiguous")
-            a.q_out, a.q_scale = q_out.data_ptr(), q_scale.data_ptr()
-            a.q_out_stride[:] = st[:3]
-        if pos is not None:
-            self._rotary(a.rotary, B, L, dev, pos, freq, axis, pairing)
+        planes = (0, 0, 0, 0, 0, 0, 0)
         if weight is not None or order is not None:
-            a.weight_stride[:] = _slots(weight, "weight", torch.float32, B, cache.Hkv, cache.capacity, dev)
-            a.order_stride[:] = _slots(order, "order", torch.int32, B, cache.Hkv, cache.capacity, dev)
             _check(first, "first", torch.int32, (B,), dev, True)
-            a.weight, a.order, a.first = _ptr(weight), _ptr(order), _ptr(first)
-        rc = self._lib.intattn_cache_append(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(dev, stream)))
-        if rc != OK:
-            raise IntAttnError(rc, self.last_error())
+            planes = (_ptr(weight), _ptr(order), _ptr(first), *_slots(weight, "weight", torch.float32, B, cache.Hkv, cache.capacity, dev),
+                      *_slots(order, "order", torch.int32, B, cache.Hkv, cache.capacity, dev))
+        args = _APPEND.pack(L, Hq, code, 0, _ptr(q), k.data_ptr(), v.data_ptr(), q0 * es, q1 * es, q2 * es, k0 * es, k1 * es, k2 * es,
+                            v0 * es, v1 * es, v2 * es, _ptr(n_new), _ptr(q_out) if Hq else 0, o0, o1, o2, _ptr(q_scale) if Hq else 0,
+                            *(_NO_ROTATION if pos is None else _rotation(B, L, dev, pos, freq, axis, pairing, False)), *planes)
+        self._done(self._lib.intattn_cache_append(self._ctx, cache._ref, args, self._stream(dev, stream)))
         return (q_out, q_scale) if q is not None else None
-
-    def _cache_forward_args(self, cache, q, scale_q, out, dtype, scale_out, n_new, max_len, weight, weight_out, decay):
-        import torch
-
-        dev, (B, Hq, L, d) = cache.device, q.shape
-        _check(q, "q", torch.int8, (cache.B, Hq, L, cache.d), dev)
-        _check(scale_q, "scale_q", torch.float32, (B, Hq, L), dev, True)
-        _check(n_new, "n_new", torch.int32, (B,), dev, True)
-        a = CacheForwardArgs()
-        types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
-        if out is None:
-            out = torch.empty((B, Hq, L, d), dtype=dtype, device=dev)
-        _check(out, "out", out.dtype, (B, Hq, L, d), dev)
-        if out.dtype not in types or q.stride(3) != 1 or out.stride(3) != 1:
-            raise ValueError("out must be float32/float16/bfloat16/int8, the head dimension contiguous")
-        if scale_out is not None:
-            a.scale_out_mode = int(scale_out.numel() > 1)
-            _check(scale_out, "scale_out", torch.float32, (Hq if a.scale_out_mode else 1,), dev, True)
-        a.Hq, a.L, a.max_len, a.out_type = Hq, L, int(max_len), types[out.dtype]
-        es = out.element_size()
-        st, so = q.stride(), out.stride()
-        a.q_stride[:] = st[:3]
-        a.out_stride[0], a.out_stride[1], a.out_stride[2] = so[0] * es, so[1] * es, so[2] * es
-        a.q, a.scale_q, a.n_new, a.out, a.scale_out = q.data_ptr(), scale_q.data_ptr(), _ptr(n_new), out.data_ptr(), _ptr(scale_out)
-        if weight is not None:
-            slots = min(cache.capacity, max_len) if max_len else cache.capacity
-            weight_out = weight if weight_out is None else weight_out
-            a.weight_stride[:] = _slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev)
-            a.weight_out_stride[:] = _slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev)
-            a.weight, a.weight_out, a.decay = weight.data_ptr(), weight_out.data_ptr(), float(decay)
-        return a, out
 
     def cache_forward(self, cache: PagedCache, q, scale_q, *, out=None, dtype=None, scale_out=None, n_new=None, max_len=0,
                       weight=None, weight_out=None, decay=1.0, stream=None):
@@ -699,13 +674,36 @@ class IntAttn:
         [B, Hkv, slots] float32: accumulated attention weight of each key, written to ``weight_out`` (default: in place)."""
         import torch
 
-        a, out = self._cache_forward_args(cache, q, scale_q, out, dtype or torch.bfloat16, scale_out, n_new, max_len, weight, weight_out, decay)
-        rc = self._lib.intattn_cache_forward(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(cache.device, stream)))
-        if rc != OK:
-            raise IntAttnError(rc, self.last_error())
+        dev, B, Hq, L, d = cache.device, cache.B, q.shape[1], q.shape[2], cache.d
+        shape = (B, Hq, L, d)
+        q0, q1, q2, _ = _rows(q, "q", torch.int8, shape, dev)
+        _check(scale_q, "scale_q", torch.float32, (B, Hq, L), dev, True)
+        _check(n_new, "n_new", torch.int32, (B,), dev, True)
+        if out is None:
+            out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=q.device)
+        code = 3 if out.dtype is torch.int8 else _float_types().get(out.dtype)
+        if code is None:
+            raise ValueError("out must be float32/float16/bfloat16/int8")
+        o0, o1, o2, _ = _rows(out, "out", out.dtype, shape, dev)
+        es = out.element_size()
+        per_head = int(scale_out is not None and scale_out.numel() > 1)
+        _check(scale_out, "scale_out", torch.float32, (Hq if per_head else 1,), dev, True)
+        planes = (0, 0, 0, 0, 0, 0)
+        if weight is not None:
+            slots = min(cache.capacity, max_len) if max_len else cache.capacity
+            weight_out = weight if weight_out is None else weight_out
+            planes = (weight.data_ptr(), weight_out.data_ptr(), *_slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev),
+                      *_slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev))
+        args = _CACHE_FORWARD.pack(Hq, L, int(max_len), code, q.data_ptr(), q0, q1, q2, scale_q.data_ptr(), _ptr(n_new), out.data_ptr(),
+                                   o0 * es, o1 * es, o2 * es, _ptr(scale_out), *planes, float(decay), per_head)
+        self._done(self._lib.intattn_cache_forward(self._ctx, cache._ref, args, self._stream(dev, stream)))
         return out
 
-    def _evict_args(self, cache, keep, weight, order, total, sink, recent, max_len, weight_out, order_out, lens_out):
+    def cache_evict(self, cache: PagedCache, keep: int, weight, *, order=None, total=None, sink=0, recent=0, max_len=0,
+                    weight_out=None, order_out=None, lens_out=None, stream=None):
+        """intattn_cache_evict: sequences longer than ``keep`` keep the keys of each head that have drawn most ``weight``
+        [B, Hkv, slots], among them the first ``sink`` and the last ``recent`` by ``order`` (int32 [B, Hkv, slots]; ``total`` [B]: tokens so
+        far).  weight, order and lens change in place unless ``*_out`` tensors are given."""
         import torch
 
         dev, B, Hkv = cache.device, cache.B, cache.Hkv
@@ -713,26 +711,13 @@ class IntAttn:
         weight_out = weight if weight_out is None else weight_out
         order_out = order if order_out is None else order_out
         lens_out = cache.lens if lens_out is None else lens_out
-        a = EvictArgs()
-        a.keep, a.sink, a.recent, a.max_len = int(keep), int(sink), int(recent), int(max_len)
-        for t, what, kind, at in ((weight, "weight", torch.float32, a.weight_stride), (weight_out, "weight_out", torch.float32, a.weight_out_stride),
-                                  (order, "order", torch.int32, a.order_stride), (order_out, "order_out", torch.int32, a.order_out_stride)):
-            at[0], at[1] = _slots(t, what, kind, B, Hkv, slots, dev)
         _check(total, "total", torch.int32, (B,), dev, True)
         _check(lens_out, "lens_out", torch.int32, (B,), dev, True)
-        a.weight, a.weight_out, a.order, a.order_out = _ptr(weight), _ptr(weight_out), _ptr(order), _ptr(order_out)
-        a.total, a.lens_out = _ptr(total), lens_out.data_ptr()
-        return a
-
-    def cache_evict(self, cache: PagedCache, keep: int, weight, *, order=None, total=None, sink=0, recent=0, max_len=0,
-                    weight_out=None, order_out=None, lens_out=None, stream=None):
-        """intattn_cache_evict: sequences longer than ``keep`` keep the keys of each head that have drawn most ``weight``
-        [B, Hkv, slots], among them the first ``sink`` and the last ``recent`` by ``order`` (int32 [B, Hkv, slots]; ``total`` [B]: tokens so
-        far).  weight, order and lens change in place unless ``*_out`` tensors are given."""
-        a = self._evict_args(cache, keep, weight, order, total, sink, recent, max_len, weight_out, order_out, lens_out)
-        rc = self._lib.intattn_cache_evict(self._ctx, ctypes.byref(cache.args), ctypes.byref(a), ctypes.c_void_p(self._stream(cache.device, stream)))
-        if rc != OK:
-            raise IntAttnError(rc, self.last_error())
+        args = _EVICT.pack(int(keep), int(sink), int(recent), int(max_len), _ptr(weight), _ptr(weight_out), _ptr(order), _ptr(order_out),
+                           *_slots(weight, "weight", torch.float32, B, Hkv, slots, dev), *_slots(weight_out, "weight_out", torch.float32, B, Hkv, slots, dev),
+                           *_slots(order, "order", torch.int32, B, Hkv, slots, dev), *_slots(order_out, "order_out", torch.int32, B, Hkv, slots, dev),
+                           _ptr(total), lens_out.data_ptr())
+        self._done(self._lib.intattn_cache_evict(self._ctx, cache._ref, args, self._stream(dev, stream)))
 
     def cache_reserve(self, cache: PagedCache, rows: int = 0, keep: int = 0, max_len: int = 0):
         """intattn_cache_reserve: room for ``cache_forward`` with up to ``rows`` = Hq / Hkv * L rows a KV head and for ``cache_evict``
