@@ -305,7 +305,7 @@ INTATTN_API int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *args, vo
  * of its L are padding: nothing is written for their K and V, their integers and scales of Q are 0.  Inputs must be finite.
  */
 typedef struct {
-    int32_t L, Hq;             /* tokens of a sequence, 1 .. 131071; query heads, a multiple of Hkv, or 0    */
+    int32_t L, Hq;             /* tokens of a sequence, 1 .. 131071; query heads, a multiple of Hkv, or 0; Hq + 2 Hkv <= 2048 */
     int32_t dtype;             /* of q, k, v: 0 = fp32, 1 = fp16, 2 = bf16                                   */
     int32_t reserved;          /* must be 0                                                                  */
     const void *q, *k, *v;     /* [B, H, L, d], BYTE strides of B, H, L, all multiples of 16; q NULL if Hq = 0 */

@@ -1,111 +1,192 @@
 // New tokens into the paged cache, for gfx950: K rotated, K and V quantized with the cache's scales into their pages, Q rotated
 // and quantized with a scale of its own for each token and head (Sec. 2.1, Eq. quant).  Every element is read once and leaves as
-// one byte; a large call is bound by HBM, a decoding step's by the latency of one launch.  A workgroup takes a few tokens with
-// all their heads (the angles of a token are evaluated once), d / 16 lanes a row, so that the maximum over a row of Q needs
-// shuffles alone.
+// one byte; a decoding step's call is bound by the latency of one launch.  A workgroup takes a few tokens with all their heads (the
+// angles of a token are evaluated once), 32 bytes of a row to a lane, so that the maximum over a row of Q needs shuffles alone.
 #include "cache_common.h"
+#include "work_map.h"
 
 namespace intattn {
 
 namespace {
 
 constexpr int ANT = 256;
+constexpr int TOKENS = 4; // of a workgroup at most
+constexpr int HEAD_BYTES = 32;
 
-// nearest integer of the IEEE fp32 quotient, ties to even, clamped
-__device__ __forceinline__ int quantized(float x, float s)
+// Integers of x: rint of the IEEE fp32 quotient x / s, ties to even, clamped to +-127.  With r the reciprocal of s to one unit in the last place, y = fma(x, r, 128) is off
+// the quotient + 128 by less than 2^-15 where that lies in a byte's range, so wherever y is farther than 2^-14 from every half-integer
+// both round alike (units with an element nearer than that take the division), and the conversion to an unsigned byte rounds to nearest
+// even and saturates: six operations an element.
+template <int N> __device__ __forceinline__ void quantize(const float (&x)[N], float s, uint32_t (&w)[N / 4])
 {
-    return (int)fminf(fmaxf(__builtin_rintf(x / s), -127.0f), 127.0f);
+    const float r = __builtin_amdgcn_rcpf(s);
+    float y[N], off = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        y[i] = __builtin_fmaf(x[i], r, 128.0f);
+        off = fmaxf(off, __builtin_fabsf(y[i] - __builtin_rintf(y[i])));
+    }
+    if (off > 0.5f - 6.103515625e-05f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = __builtin_rintf(x[i] / s) + 128.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        uint32_t q = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q = __builtin_amdgcn_cvt_pk_u8_f32(fmaxf(y[4 * i + j], 1.0f), j, q); // (-127 the least)
+        w[i] = q ^ 0x80808080u;
+    }
 }
 
-template <int D, int DTYPE> __global__ __launch_bounds__(ANT) void append_kernel(const AppendParams p)
+template <int D, int DTYPE, bool HALVES> __global__ __launch_bounds__(ANT) void append_kernel(const AppendParams p)
 {
-    constexpr int UNITS = D / 16;
-    extern __shared__ double2 turns[]; // [tokens][rot / 2]
-    const int pairs = p.r.rot / 2;
-    const int64_t all = (int64_t)p.c.B * p.L, t0 = (int64_t)blockIdx.x * p.tokens;
-    const int n = (int)min((int64_t)p.tokens, all - t0);
-    for (int i = threadIdx.x; i < n * pairs; i += ANT) {
-        const int64_t t = t0 + i / pairs;
-        turns[i] = turn_of(p.r, (int)(t / p.L), (int)(t % p.L), i % pairs);
+    constexpr int N = HALF<DTYPE>, UNITS = D / (2 * N), ROWS = ANT / UNITS;
+    // What the rows of a token, and those of a head, share is formed once (with three strides of each of three tensors in every row the
+    // kernel was bound by vector instructions, 390 to a unit, and loads of a row waited behind those of the next).
+    struct Token {
+        int64_t src[3], dst[3]; // Q, K, V: offset of the row of head 0; dst < 0: nothing is written
+        int b, l, slot, order;
+        bool there;
+    };
+    struct Head {
+        const uint8_t *src;
+        int8_t *dst;
+        float scale; // K, V
+        int which, head;
+    };
+    static_assert(sizeof(Head) <= HEAD_BYTES, "room for the heads");
+    extern __shared__ char lds[]; // heads, turns [tokens][rot / 2]
+    __shared__ Token token[TOKENS];
+    Head *const head = (Head *)lds; // HEAD_BYTES apart
+    double2 *const turns = (double2 *)(lds + p.turns_at);
+    const int pairs = p.r.rot / 2, t0 = blockIdx.x * p.tokens, n = min(p.tokens, p.c.B * p.L - t0), rows = n * p.heads;
+    const int u = threadIdx.x % UNITS;
+    const Unit plain = unit_of<DTYPE, HALVES>(u, D, 0), turned = unit_of<DTYPE, HALVES>(u, D, p.r.rot);
+    for (int h = threadIdx.x; h < p.heads; h += ANT) {
+        const int which = h < p.Hq ? 0 : h < p.Hq + p.c.Hkv ? 1 : 2, at = h - (which == 0 ? 0 : which == 1 ? p.Hq : p.Hq + p.c.Hkv);
+        Head to;
+        to.src = p.x[which] + at * p.xs[which][1];
+        to.dst = which == 0 ? p.q_out + at * p.qos[1] : which == 1 ? p.c.k + at * p.c.ks[1] : p.c.v + at * p.c.vs[1];
+        to.scale = (which == 2 ? p.c.scale_v : p.c.scale_k)[p.c.per_head && which > 0 ? at : 0];
+        to.which = which;
+        to.head = at;
+        head[h] = to;
+    }
+    if ((int)threadIdx.x >= ANT - n) { // (other threads than those with the first heads)
+        const int i = threadIdx.x - (ANT - n), b = quotient(t0 + i, p.by_L), l = t0 + i - b * p.L;
+        const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), slot = len - fresh + l;
+        Token to;
+        to.b = b;
+        to.l = l;
+        to.slot = slot;
+        to.there = l < fresh;
+        to.order = p.first ? p.first[b] + l : slot;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) to.src[w] = b * p.xs[w][0] + l * p.xs[w][2];
+        to.dst[0] = b * p.qos[0] + l * p.qos[2];
+        to.dst[1] = to.dst[2] = -1;
+        if (to.there) {
+            const Slot at = find_slot(p.c, p.c.table + b * p.c.table_stride, slot);
+            if (at.page >= 0) {
+                to.dst[1] = at.page * p.c.ks[0] + at.at * p.c.ks[2];
+                to.dst[2] = at.page * p.c.vs[0] + at.at * p.c.vs[2];
+            }
+        }
+        token[i] = to;
+    }
+    for (int k = threadIdx.x; k < n * pairs; k += ANT) {
+        const int t = quotient(k, p.by_pairs), b = quotient(t0 + t, p.by_L);
+        turns[k] = turn_of(p.r, b, t0 + t - b * p.L, k - t * pairs);
     }
     __syncthreads();
-    const int heads = p.Hq + 2 * p.c.Hkv, rows = n * heads;
-    const int u = threadIdx.x % UNITS;
-    for (int row0 = 0; row0 < rows; row0 += ANT / UNITS) {
-        const int row = row0 + threadIdx.x / UNITS;
-        if (row >= rows) break; // all lanes of a row alike
-        const int t = row / heads, h = row % heads;
-        const int b = (int)((t0 + t) / p.L), l = (int)((t0 + t) % p.L);
-        const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len);
-        const int which = h < p.Hq ? 0 : h < p.Hq + p.c.Hkv ? 1 : 2, head = h - (which == 0 ? 0 : which == 1 ? p.Hq : p.Hq + p.c.Hkv);
-        const bool there = l < fresh;
-        const bool rotated = which < 2 && 16 * u < p.r.rot;
-        const Unit un = unit_of(u, which < 2 ? p.r.rot : 0, p.r.halves);
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-        if (there) {
-            const Raw16<DTYPE> raw = load_unit<DTYPE>(p.x[which] + b * p.xs[which][0] + head * p.xs[which][1] + l * p.xs[which][2], un);
-            widen_unit<DTYPE>(raw, un, rotated, turns + t * pairs, u, x);
-        }
-        float scale;
-        int8_t *dst = nullptr;
-        if (which == 0) {
+    struct Row {
+        int t, h, which;
+        Raw raw;
+    };
+    auto ask = [&](int i) {
+        Row r;
+        r.t = quotient(i, p.by_heads);
+        r.h = i - r.t * p.heads;
+        r.which = head[r.h].which;
+        r.raw = load_unit<DTYPE>(head[r.h].src + token[r.t].src[r.which], r.which < 2 ? turned : plain);
+        return r;
+    };
+    const int step = ROWS * gridDim.y;
+    int i = threadIdx.x / UNITS + blockIdx.y * ROWS;
+    if (i >= rows) return;
+    Row next = ask(i);
+    while (i < rows) { // all lanes of a row alike
+        const Row r = next;
+        const Unit un = r.which < 2 ? turned : plain;
+        float x[2 * N];
+        widen<DTYPE>(r.raw, x);
+        i += step;
+        if (i < rows) next = ask(i);
+        const Token &at = token[r.t];
+        const Head &to = head[r.h];
+        if (r.which < 2) turn_unit<DTYPE, HALVES>(x, turned, turns + r.t * pairs);
+        float scale = to.scale;
+        const int64_t place = at.dst[r.which];
+        if (r.which == 0) {
             float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, __builtin_fabsf(x[i]));
+            for (int j = 0; j < 2 * N; ++j) {
+                if (!at.there) x[j] = 0.0f; // padding
+                m = fmaxf(m, __builtin_fabsf(x[j]));
+            }
 #pragma unroll
             for (int o = 1; o < UNITS; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
             scale = fmaxf(m, 1e-12f) / 127.0f;
-            if (u == 0) p.q_scale[((int64_t)b * p.Hq + head) * p.L + l] = there ? scale : 0.0f;
-            dst = p.q_out + b * p.qos[0] + head * p.qos[1] + l * p.qos[2];
-        } else {
-            scale = (which == 1 ? p.c.scale_k : p.c.scale_v)[p.c.per_head ? head : 0];
-            const int slot = len - fresh + l;
-            if (there) {
-                const Slot at = find_slot(p.c, p.c.table + b * p.c.table_stride, slot);
-                if (at.page >= 0) {
-                    const int64_t *s = which == 1 ? p.c.ks : p.c.vs;
-                    dst = (which == 1 ? p.c.k : p.c.v) + at.page * s[0] + head * s[1] + at.at * s[2];
-                }
-                if (which == 1 && u == 0) {
-                    if (p.weight) p.weight[b * p.wst[0] + head * p.wst[1] + slot] = 0.0f;
-                    if (p.order) p.order[b * p.ost[0] + head * p.ost[1] + slot] = p.first ? p.first[b] + l : slot;
-                }
-            }
+            if (u == 0) p.q_scale[((int64_t)at.b * p.Hq + to.head) * p.L + at.l] = at.there ? scale : 0.0f;
+        } else if (r.which == 1 && u == 0 && at.there) {
+            if (p.weight) p.weight[at.b * p.wst[0] + to.head * p.wst[1] + at.slot] = 0.0f;
+            if (p.order) p.order[at.b * p.ost[0] + to.head * p.ost[1] + at.slot] = at.order;
         }
-        if (!dst) continue;
-        const bool ok = good_cache_scale(scale);
-        uint32_t w[4] = {0, 0, 0, 0};
+        if (place < 0) continue;
+        int8_t *const dst = to.dst + place;
+        uint32_t w[N / 2];
+        quantize<2 * N>(x, scale, w);
+        if (!good_cache_scale(scale)) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t a = ok ? (uint32_t)quantized(x[2 * j], scale) & 0xffu : 0u, c = ok ? (uint32_t)quantized(x[2 * j + 1], scale) & 0xffu : 0u;
-            const int i0 = un.halves ? j : 2 * j, i1 = un.halves ? 8 + j : 2 * j + 1; // in memory order
-            w[0] |= i0 / 4 == 0 ? a << (8 * (i0 % 4)) : 0u;
-            w[1] |= i0 / 4 == 1 ? a << (8 * (i0 % 4)) : 0u;
-            w[2] |= i0 / 4 == 2 ? a << (8 * (i0 % 4)) : 0u;
-            w[3] |= i0 / 4 == 3 ? a << (8 * (i0 % 4)) : 0u;
-            w[0] |= i1 / 4 == 0 ? c << (8 * (i1 % 4)) : 0u;
-            w[1] |= i1 / 4 == 1 ? c << (8 * (i1 % 4)) : 0u;
-            w[2] |= i1 / 4 == 2 ? c << (8 * (i1 % 4)) : 0u;
-            w[3] |= i1 / 4 == 3 ? c << (8 * (i1 % 4)) : 0u;
+            for (int j = 0; j < N / 2; ++j) w[j] = 0;
         }
-        *(uint2 *)(dst + un.first) = make_uint2(w[0], w[1]);
-        *(uint2 *)(dst + un.second) = make_uint2(w[2], w[3]);
+        if constexpr (N == 8) {
+            *(uint2 *)(dst + un.first) = make_uint2(w[0], w[1]);
+            *(uint2 *)(dst + un.second) = make_uint2(w[2], w[3]);
+        } else {
+            *(uint32_t *)(dst + un.first) = w[0];
+            *(uint32_t *)(dst + un.second) = w[1];
+        }
     }
 }
 
 } // namespace
 
+template <int D, bool HALVES> static auto append_kernel_of(int dtype)
+{
+    return dtype == 0 ? append_kernel<D, 0, HALVES> : dtype == 1 ? append_kernel<D, 1, HALVES> : append_kernel<D, 2, HALVES>;
+}
+
 int launch_append(const AppendParams &p_, int d, int dtype, void *stream)
 {
     AppendParams p = p_;
-    p.tokens = 1;
-    const int64_t blocks = ((int64_t)p.c.B * p.L + p.tokens - 1) / p.tokens;
-    const size_t lds = sizeof(double2) * (size_t)p.tokens * (size_t)(p.r.rot / 2);
-    void (*kernel)(const AppendParams) = d == 64 ? (dtype == 0 ? append_kernel<64, 0> : dtype == 1 ? append_kernel<64, 1> : append_kernel<64, 2>)
-                                                 : (dtype == 0 ? append_kernel<128, 0> : dtype == 1 ? append_kernel<128, 1> : append_kernel<128, 2>);
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(ANT), lds, (hipStream_t)stream, p);
+    const int64_t all = (int64_t)p.c.B * p.L;
+    p.heads = p.Hq + 2 * p.c.Hkv;
+    p.by_heads = fast_div((uint32_t)p.heads);
+    p.by_L = fast_div((uint32_t)p.L);
+    p.by_pairs = fast_div((uint32_t)(p.r.rot > 0 ? p.r.rot / 2 : 1));
+    // tokens of a workgroup: two to three rounds of its lanes where there are tokens enough (8192 tokens, us: d 128, 48 heads, one token 49.5, two
+    // 44.0, four 44.6, eight 47.2; d 64, 48 heads 34.6, 28.3, 25.9, 25.1); the heads of a token over several workgroups where there are few
+    const int units = d / (dtype == 0 ? 8 : 16), rows = ANT / units;
+    p.tokens = all >= 1024 ? std::min(TOKENS, std::max(1, 768 / (p.heads * units))) : 1;
+    const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.heads + rows - 1) / rows;
+    const int64_t parts = blocks >= 512 ? 1 : std::min<int64_t>(rounds, std::max<int64_t>(1, 512 / blocks));
+    p.turns_at = p.heads * HEAD_BYTES;
+    const size_t lds = (size_t)p.turns_at + sizeof(double2) * (size_t)p.tokens * (size_t)(p.r.rot / 2);
+    void (*kernel)(const AppendParams) = d == 64 ? (p.r.halves ? append_kernel_of<64, true>(dtype) : append_kernel_of<64, false>(dtype))
+                                                 : (p.r.halves ? append_kernel_of<128, true>(dtype) : append_kernel_of<128, false>(dtype));
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks, (uint32_t)parts), dim3(ANT), lds, (hipStream_t)stream, p);
     return (int)hipGetLastError();
 }
 

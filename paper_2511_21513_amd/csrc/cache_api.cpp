@@ -282,7 +282,7 @@ int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cache, const int
         if (a->L < 1 || a->Hq < 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "L must be >= 1 and Hq >= 0");
         if (a->L > MOST_KEYS) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "L must not exceed 131071");
         if (a->Hq % cache->Hkv != 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "Hq must be a multiple of Hkv");
-        if (a->Hq > 65535) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "more than 65535 query heads");
+        if ((int64_t)a->Hq + 2 * (int64_t)cache->Hkv > 2048) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "Hq + 2 Hkv must not exceed 2048");
         if ((int64_t)cache->B * a->L > 2147483647LL) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "B * L must not exceed 2^31-1");
         if (a->dtype < 0 || a->dtype > 2) return fail(ctx, INTATTN_ERR_INVALID_ARG, "dtype must be 0 (fp32), 1 (fp16) or 2 (bf16)");
         if (a->reserved != 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "reserved must be 0");

@@ -27,44 +27,56 @@ __device__ __forceinline__ Slot find_slot(const CacheParams &c, const int32_t *r
     return Slot{(uint32_t)page < (uint32_t)c.n_pages ? page : -1, slot - n * c.page_size};
 }
 
-// ------------------------------------------------------------------ rows in lanes of sixteen elements
-// A lane takes 16 channels of a row: 16 u .. 16 u + 15, or, where the rotation pairs channel i with i + rot / 2, the eight pairs
-// from i = 8 u on.  Pairs sit next to each other in x, so x[2 j], x[2 j + 1] are turned by the angle of pair 8 u + j in either
-// layout.  Channels from rot on are in order in both.
+// ------------------------------------------------------------------ rows in lanes
+// A lane takes 32 bytes of a row, two runs of HALF channels: HALF u and on of either half of the row, or, where the rotation pairs
+// channel i with i + rot / 2, of either half of the rotated channels (so that a lane has both of each pair) and then of the others.
+// The runs of neighbouring lanes follow each other: 32 bytes in one piece to a lane took a twentieth longer.
+template <int DTYPE> constexpr int HALF = DTYPE == 0 ? 4 : 8;
+
 struct Unit {
-    int first, second; // channel of the first eight elements in memory and of the other eight
-    bool halves;       // pairs straddle the two
+    int first, second;    // channels where the two runs start
+    bool turn[2];         // whether they are rotated
 };
-__device__ __forceinline__ Unit unit_of(int u, int rot, bool halves)
+// rot: rotated channels of this row (0: none)
+template <int DTYPE, bool HALVES> __device__ __forceinline__ Unit unit_of(int u, int d, int rot)
 {
-    const bool split = halves && 16 * u < rot;
-    return Unit{split ? 8 * u : 16 * u, split ? rot / 2 + 8 * u : 16 * u + 8, split};
+    constexpr int N = HALF<DTYPE>;
+    const int at = N * u;
+    if constexpr (HALVES) {
+        const bool in = 2 * at < rot;
+        return Unit{in ? at : rot / 2 + at, in ? rot / 2 + at : d / 2 + at, {in, in}};
+    } else {
+        return Unit{at, d / 2 + at, {at < rot, d / 2 + at < rot}};
+    }
 }
 
-template <int DTYPE> struct Raw16 {
-    uint4 v[DTYPE == 0 ? 4 : 2];
+struct Raw {
+    v4i v[2];
 };
-template <int DTYPE> __device__ __forceinline__ Raw16<DTYPE> load_unit(const uint8_t *row, const Unit &u)
+template <int DTYPE> __device__ __forceinline__ Raw load_unit(const uint8_t *row, const Unit &u)
 {
-    constexpr int ES = DTYPE == 0 ? 4 : 2, N = DTYPE == 0 ? 2 : 1;
-    Raw16<DTYPE> r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        r.v[i] = *(const uint4 *)(row + (int64_t)u.first * ES + 16 * i);
-        r.v[N + i] = *(const uint4 *)(row + (int64_t)u.second * ES + 16 * i);
-    }
-    return r;
+    constexpr int ES = DTYPE == 0 ? 4 : 2;
+    return Raw{__builtin_nontemporal_load((const v4i *)(row + u.first * ES)), __builtin_nontemporal_load((const v4i *)(row + u.second * ES))};
 }
-// element i of the unit in memory order, in fp32 (exact)
-template <int DTYPE> __device__ __forceinline__ float raw_element(const Raw16<DTYPE> &r, int i)
+// the elements in memory order, in fp32 (exact)
+template <int DTYPE> __device__ __forceinline__ void widen(const Raw &r, float (&x)[2 * HALF<DTYPE>])
 {
-    constexpr int PER = DTYPE == 0 ? 4 : 8;
-    const uint4 v = r.v[i / PER];
-    const int j = i % PER;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if constexpr (DTYPE == 0) return __uint_as_float(w[j]);
-    else if constexpr (DTYPE == 1) return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[j / 2] >> (16 * (j & 1))));
-    else return __uint_as_float((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w[4] = {(uint32_t)r.v[h][0], (uint32_t)r.v[h][1], (uint32_t)r.v[h][2], (uint32_t)r.v[h][3]};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DTYPE == 0) {
+                x[4 * h + i] = __uint_as_float(w[i]);
+            } else if constexpr (DTYPE == 1) {
+                x[8 * h + 2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] & 0xffffu));
+                x[8 * h + 2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
+            } else {
+                x[8 * h + 2 * i] = __uint_as_float(w[i] << 16);
+                x[8 * h + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------ rotation
@@ -79,29 +91,28 @@ __device__ __forceinline__ double2 turn_of(const RotaryParams &r, int b, int l, 
     return make_double2(c, r.inverse ? -s : s);
 }
 
-// Both results in 64 bits, rounded once: a rotated row does not depend on how products are joined, and the integers that are made
-// of it later are the definition's.
+// A unit's pairs turned; turns: those of the token's pairs.  Both results in 64 bits, rounded once: a rotated row does not depend on how
+// products are joined, and the integers that are made of it later are the definition's.
 __device__ __forceinline__ void turn_pair(float &a, float &b, const double2 t)
 {
     const double x = a, y = b;
     a = (float)(x * t.x - y * t.y);
     b = (float)(x * t.y + y * t.x);
 }
-
-// x in pair order from a unit in memory, turned if the unit is rotated; turns: those of the token's pairs
-template <int DTYPE>
-__device__ __forceinline__ void widen_unit(const Raw16<DTYPE> &raw, const Unit &un, bool rotated, const double2 *turns, int u, float (&x)[16])
+template <int DTYPE, bool HALVES> __device__ __forceinline__ void turn_unit(float (&x)[2 * HALF<DTYPE>], const Unit &un, const double2 *turns)
 {
+    constexpr int N = HALF<DTYPE>;
+    if constexpr (HALVES) {
+        if (!un.turn[0]) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float e0 = raw_element<DTYPE>(raw, 2 * j), e1 = raw_element<DTYPE>(raw, 2 * j + 1);
-        const float h0 = raw_element<DTYPE>(raw, j), h1 = raw_element<DTYPE>(raw, 8 + j);
-        x[2 * j] = un.halves ? h0 : e0;
-        x[2 * j + 1] = un.halves ? h1 : e1;
-    }
-    if (rotated) {
+        for (int j = 0; j < N; ++j) turn_pair(x[j], x[N + j], turns[un.first + j]);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) turn_pair(x[2 * j], x[2 * j + 1], turns[8 * u + j]);
+        for (int h = 0; h < 2; ++h) {
+            if (!un.turn[h]) continue;
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) turn_pair(x[N * h + 2 * j], x[N * h + 2 * j + 1], turns[(h ? un.second : un.first) / 2 + j]);
+        }
     }
 }
 

@@ -34,6 +34,8 @@ struct RopeParams {
     int32_t H0, H;             // heads of the first tensor, of both
     int32_t B, L, d;
     int32_t tokens;            // of a workgroup
+    int32_t units, per_token;  // 32-byte units of a row, of a token
+    FastDiv by_token, by_units, by_pairs, by_L;
     RotaryParams r;
 };
 
@@ -41,8 +43,10 @@ struct AppendParams {
     CacheParams c;
     const uint8_t *x[3];       // q, k, v
     int64_t xs[3][3];
-    int32_t Hq, L;
+    int32_t Hq, L, heads;      // heads: of Q, K and V
     int32_t tokens;            // of a workgroup
+    int32_t turns_at;          // bytes of LDS in front of the turns
+    FastDiv by_heads, by_L, by_pairs;
     const int32_t *n_new;
     int8_t *q_out;
     int64_t qos[3];

@@ -2,8 +2,9 @@
 //   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = pos[axis] * freq,
 // for each pair of a row's first `rot` channels.  Every element is read and written once, so a large call is bound by HBM.  A
 // workgroup takes a few tokens with all their heads, so that the angles of a token, which all heads share, are evaluated once
-// (in 64 bits: cache_common.h) and lie in LDS.
+// (in 64 bits: cache_common.h) and lie in LDS; the first rows are asked for before.
 #include "cache_common.h"
+#include "work_map.h"
 
 namespace intattn {
 
@@ -11,62 +12,70 @@ namespace {
 
 constexpr int RNT = 256;
 
-template <int DTYPE> __device__ __forceinline__ void store_unit(uint8_t *row, const Unit &un, const float (&x)[16])
+template <int DTYPE> __device__ __forceinline__ void store_unit(uint8_t *row, const Unit &un, const float (&x)[2 * HALF<DTYPE>])
 {
-    constexpr int ES = DTYPE == 0 ? 4 : 2;
-    float m[16]; // in memory order
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        m[j] = un.halves ? x[2 * j] : x[j];
-        m[8 + j] = un.halves ? x[2 * j + 1] : x[8 + j];
-    }
+    constexpr int ES = DTYPE == 0 ? 4 : 2, N = HALF<DTYPE>;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint8_t *at = row + (int64_t)(h ? un.second : un.first) * ES;
-        if constexpr (DTYPE == 0) {
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                *(float4 *)(at + 16 * i) = make_float4(m[8 * h + 4 * i], m[8 * h + 4 * i + 1], m[8 * h + 4 * i + 2], m[8 * h + 4 * i + 3]);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint16_t lo, hi;
-                if constexpr (DTYPE == 1) {
-                    lo = __builtin_bit_cast(uint16_t, (_Float16)m[8 * h + 2 * i]);
-                    hi = __builtin_bit_cast(uint16_t, (_Float16)m[8 * h + 2 * i + 1]);
-                } else {
-                    lo = __builtin_bit_cast(uint16_t, (__bf16)m[8 * h + 2 * i]);
-                    hi = __builtin_bit_cast(uint16_t, (__bf16)m[8 * h + 2 * i + 1]);
-                }
-                w[i] = (uint32_t)lo | ((uint32_t)hi << 16);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DTYPE == 0) {
+                w[i] = __float_as_uint(x[N * h + i]);
+            } else if constexpr (DTYPE == 1) {
+                w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[N * h + 2 * i]) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[N * h + 2 * i + 1]) << 16);
+            } else {
+                w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[N * h + 2 * i]) | ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[N * h + 2 * i + 1]) << 16);
             }
-            *(uint4 *)at = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        // (past the caches: Q and K of 8192 tokens, bf16, 40 heads, 36.0 -> 31.1 us)
+        __builtin_nontemporal_store(v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]}, (v4i *)(row + (h ? un.second : un.first) * ES));
     }
 }
 
-template <int DTYPE> __global__ __launch_bounds__(RNT) void rope_kernel(const RopeParams p)
+template <int DTYPE, bool HALVES> __global__ __launch_bounds__(RNT) void rope_kernel(const RopeParams p)
 {
+    constexpr int N = HALF<DTYPE>;
     extern __shared__ double2 turns[]; // [tokens][rot / 2]
-    const int pairs = p.r.rot / 2;
-    const int64_t all = (int64_t)p.B * p.L, t0 = (int64_t)blockIdx.x * p.tokens;
-    const int n = (int)min((int64_t)p.tokens, all - t0);
-    for (int i = threadIdx.x; i < n * pairs; i += RNT) {
-        const int64_t t = t0 + i / pairs;
-        turns[i] = turn_of(p.r, (int)(t / p.L), (int)(t % p.L), i % pairs);
+    const int pairs = p.r.rot / 2, t0 = blockIdx.x * p.tokens, n = min(p.tokens, p.B * p.L - t0);
+    const int items = n * p.per_token;
+    struct Item {
+        Unit un;
+        int64_t src, dst; // offsets in tensor w
+        int w, t;
+    };
+    auto item = [&](int i) {
+        Item it;
+        it.t = quotient(i, p.by_token);
+        const int in = i - it.t * p.per_token, h = quotient(in, p.by_units);
+        it.w = h >= p.H0;
+        const int head = h - (it.w ? p.H0 : 0), b = quotient(t0 + it.t, p.by_L), l = t0 + it.t - b * p.L;
+        it.un = unit_of<DTYPE, HALVES>(in - h * p.units, p.d, p.r.rot);
+        const int64_t *s = p.ss[it.w], *d = p.ds[it.w];
+        it.src = b * s[0] + head * s[1] + l * s[2];
+        it.dst = b * d[0] + head * d[1] + l * d[2];
+        return it;
+    };
+    int i = threadIdx.x + blockIdx.y * RNT;
+    Item it = item(min(i, items - 1));
+    Raw raw = load_unit<DTYPE>(p.src[it.w] + it.src, it.un);
+    for (int k = threadIdx.x; k < n * pairs; k += RNT) {
+        const int t = quotient(k, p.by_pairs), b = quotient(t0 + t, p.by_L);
+        turns[k] = turn_of(p.r, b, t0 + t - b * p.L, k - t * pairs);
     }
     __syncthreads();
-    const int units = p.d / 16, items = n * p.H * units;
-    for (int i = threadIdx.x; i < items; i += RNT) {
-        const int u = i % units, row = i / units, h = row % p.H, t = row / p.H;
-        const int b = (int)((t0 + t) / p.L), l = (int)((t0 + t) % p.L);
-        const int w = h >= p.H0, head = h - (w ? p.H0 : 0);
-        const Unit un = unit_of(u, p.r.rot, p.r.halves);
-        const Raw16<DTYPE> raw = load_unit<DTYPE>(p.src[w] + b * p.ss[w][0] + head * p.ss[w][1] + l * p.ss[w][2], un);
-        float x[16];
-        widen_unit<DTYPE>(raw, un, 16 * u < p.r.rot, turns + t * pairs, u, x);
-        store_unit<DTYPE>(p.dst[w] + b * p.ds[w][0] + head * p.ds[w][1] + l * p.ds[w][2], un, x);
+    const int step = RNT * gridDim.y;
+    while (i < items) {
+        float x[2 * N];
+        widen<DTYPE>(raw, x);
+        const Item now = it;
+        i += step;
+        if (i < items) {
+            it = item(i);
+            raw = load_unit<DTYPE>(p.src[it.w] + it.src, it.un);
+        }
+        turn_unit<DTYPE, HALVES>(x, now.un, turns + now.t * pairs);
+        store_unit<DTYPE>(p.dst[now.w] + now.dst, now.un, x);
     }
 }
 
@@ -76,11 +85,21 @@ int launch_rope(const RopeParams &p_, int dtype, void *stream)
 {
     RopeParams p = p_;
     const int64_t all = (int64_t)p.B * p.L;
-    p.tokens = 1;
-    const int64_t blocks = (all + p.tokens - 1) / p.tokens;
+    p.units = p.d / (dtype == 0 ? 8 : 16);
+    p.per_token = p.H * p.units;
+    p.by_token = fast_div((uint32_t)p.per_token);
+    p.by_units = fast_div((uint32_t)p.units);
+    p.by_pairs = fast_div((uint32_t)(p.r.rot / 2));
+    p.by_L = fast_div((uint32_t)p.L);
+    // tokens of a workgroup: one or two rounds of its lanes where there are tokens enough (8192 tokens of 40 heads, d 128, us: fp32, one 59.4, four
+    // 68.2; bf16, one 34.0, two 32.2, four 33.0); the heads of a token over several workgroups where there are few tokens
+    p.tokens = all >= 1024 && p.per_token < 512 ? 2 : 1;
+    const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.per_token + RNT - 1) / RNT;
+    const int64_t parts = blocks >= 512 ? 1 : std::min<int64_t>(rounds, std::max<int64_t>(1, 512 / blocks));
     const size_t lds = sizeof(double2) * (size_t)p.tokens * (size_t)(p.r.rot / 2);
-    void (*kernel)(const RopeParams) = dtype == 0 ? rope_kernel<0> : dtype == 1 ? rope_kernel<1> : rope_kernel<2>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(RNT), lds, (hipStream_t)stream, p);
+    void (*kernel)(const RopeParams) = p.r.halves ? (dtype == 0 ? rope_kernel<0, true> : dtype == 1 ? rope_kernel<1, true> : rope_kernel<2, true>)
+                                                  : (dtype == 0 ? rope_kernel<0, false> : dtype == 1 ? rope_kernel<1, false> : rope_kernel<2, false>);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks, (uint32_t)parts), dim3(RNT), lds, (hipStream_t)stream, p);
     return (int)hipGetLastError();
 }
 

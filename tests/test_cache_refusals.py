@@ -154,7 +154,7 @@ def test_long_sequences_need_a_bound(ia):
 
 
 @pytest.mark.parametrize("want, kw", [
-    (BAD, dict(L=0)), (NOT, dict(L=131072)), (BAD, dict(Hq=-4)), (BAD, dict(Hq=6)), (NOT, dict(Hq=65536)), (BAD, dict(dtype=3)), (BAD, dict(dtype=-1)), (BAD, dict(reserved=1)),
+    (BAD, dict(L=0)), (NOT, dict(L=131072)), (BAD, dict(Hq=-4)), (BAD, dict(Hq=6)), (NOT, dict(Hq=2044)), (BAD, dict(dtype=3)), (BAD, dict(dtype=-1)), (BAD, dict(reserved=1)),
     (BAD, dict(k=None)), (BAD, dict(v=None)), (BAD, dict(q=None)), (BAD, dict(q_out=None)), (BAD, dict(q_scale=None)), (BAD, dict(rot=dict(inverse=1))), (BAD, dict(k=P + 8)),
     (BAD, dict(v_stride=(2, 24))), (BAD, dict(q_out_stride=(1, 72))), (BAD, dict(q_scale=P + 2)), (BAD, dict(n_new=P + 1)), (BAD, dict(order=P + 2)), (BAD, dict(weight=P, weight_stride=(0, -1))),
 ])
