@@ -205,15 +205,13 @@ template <int D> __device__ __forceinline__ void step_scores(const v4i (&a)[4][D
         for (int i = 0; i < 4; ++i) sc[ii][i] = 4 * ii + i < left && ((seen[i] >> ii) & 1u) ? sc[ii][i] : HIDDEN;
 }
 
-// the table index of four scores (bytes of the result), and the sum of their entries
-__device__ __forceinline__ uint32_t four_indices(const int4 x, int top, int c_int, double factor, const uint8_t *entry, int &sum)
+// the table index of four distances from the row's maximum (bytes of the result), and the sum of their entries
+__device__ __forceinline__ uint32_t four_indices(const uint32_t (&away)[4], int c_int, double factor, const uint8_t *entry, int &sum)
 {
-    const int sc[4] = {x.x, x.y, x.z, x.w};
     uint32_t word = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t away = min((uint32_t)top - (uint32_t)sc[i], (uint32_t)c_int);
-        const uint32_t idx = (uint32_t)(int)__builtin_fma((double)(int)away, factor, 0.5);
+        const uint32_t idx = (uint32_t)(int)__builtin_fma((double)(int)min(away[i], (uint32_t)c_int), factor, 0.5);
         sum += entry[idx];
         word |= idx << (8 * i);
     }

@@ -1,9 +1,11 @@
 // Attention of the newest tokens over a paged INT8 cache (the pipeline of include/intattn.h, steps 1 to 8), for gfx950.
 //
 // IndexSoftmax needs the exact row maximum before any index and the exact row sum before any probability, so a row's keys are met
-// three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  (What does not fit goes to
-// attend_split.hip.)  A workgroup takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens at a
-// time; its waves take every NW-th step of 64 keys and meet at the maxima and at the sums.
+// three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  Steps whose scores do not
+// fit have room for their indices there, and K of these is read again for them: with 32 sequences of 4000 to 12400 keys, 8 KV heads of
+// four rows and d 128, 135 us, 4.2 TB/s of the bytes that have to move (the three launches of attend_split.hip 144).  A workgroup
+// takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens at a time; its waves take every NW-th step of
+// 64 keys and meet at the maxima and at the sums.
 #include "attend_common.h"
 
 #include <algorithm>
@@ -22,8 +24,10 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     __shared__ int row_max[16], row_sum[16], acc_sum[16 * ACC_ROW];
     __shared__ uint8_t entry[64], prob[16][PROB]; // LUT_hat, and P_hat of each index in a row
     __shared__ float share[16][64];             // E / S
+    // of each lane that has a row, for step after step: sixteen scores, then indices in the place of the first four; from step
+    // p.held_steps on, indices alone
+    extern __shared__ int4 held[];
     __shared__ int4 widx[NW][64];               // indices of a wave's step
-    extern __shared__ int4 held[];              // the sixteen scores, then indices, of each lane that has a row, step after step
 
     const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
@@ -31,7 +35,11 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
     const int held_rows = min(p.rows, 16);
     float *const weight_out = p.weight ? p.weight_out + b * p.wost[0] + kvh * p.wost[1] : nullptr;
-    auto place = [&](int s) { return held + 4 * ((s * 4 + kb) * held_rows + n); };
+    const int held_to = min(steps, p.held_steps);
+    auto place = [&](int s) { // the lane's
+        const int i = (s * 4 + kb) * held_rows + n;
+        return held + (s < held_to ? 4 * i : i + 3 * held_to * 4 * held_rows);
+    };
     if (steps == 0) { // no keys: zeros
         for (int i = threadIdx.x; i < p.rows * D; i += 64 * NW) store_out(p, 0.0f, 0, 31, out_row(p, b, kvh, i / D), i % D, 0);
         return;
@@ -92,7 +100,7 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
             step_scores<D>(ka, kt, qf, limit - (s * 64 + 16 * kb), kb, sc);
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
-            if (mine) {
+            if (mine && s < held_to) {
                 int4 *at = place(s);
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii) at[ii] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
@@ -127,17 +135,44 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
 
         // indices and row sums: sixteen scores of a row to a thread, whichever wave they came from, so that all lanes have work
         // (by the lanes that hold the rows it took 20 us of 115 at four rows and 8192 keys)
-        for (int i = threadIdx.x; i < steps * 4 * held_rows; i += 64 * NW) {
+        for (int i = threadIdx.x; i < held_to * 4 * held_rows; i += 64 * NW) {
             const int r = i % held_rows;
             int4 *const at = held + 4 * i;
-            const int c_int = rowp[r].c_int, row_top = row_max[r];
+            const int c_int = rowp[r].c_int;
+            const uint32_t row_top = (uint32_t)row_max[r];
             const double factor = rowp[r].factor;
             int sum = 0;
             uint32_t word[4];
 #pragma unroll
-            for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(at[ii], row_top, c_int, factor, entry, sum);
+            for (int ii = 0; ii < 4; ++ii) {
+                const int4 x = at[ii];
+                const uint32_t away[4] = {row_top - (uint32_t)x.x, row_top - (uint32_t)x.y, row_top - (uint32_t)x.z, row_top - (uint32_t)x.w};
+                word[ii] = four_indices(away, c_int, factor, entry, sum);
+            }
             at[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
             atomicAdd(&row_sum[r], sum);
+        }
+        if (held_to < steps) {
+            const int c_int = rowp[n].c_int;
+            const uint32_t row_top = (uint32_t)row_max[n];
+            const double factor = rowp[n].factor;
+            int sum = 0;
+            PlaceK at = keys.find_k(held_to + wave, lane);
+            for (int s = held_to + wave; s < steps; s += NW) {
+                v4i sc[4];
+                keys.load_k(at, lane, a[0], there[0]);
+                at = keys.find_k(s + NW, lane);
+                step_scores<D>(a[0], there[0], qf, limit - (s * 64 + 16 * kb), kb, sc);
+                if (!mine) continue;
+                uint32_t word[4];
+#pragma unroll
+                for (int ii = 0; ii < 4; ++ii) {
+                    const uint32_t away[4] = {row_top - (uint32_t)sc[ii][0], row_top - (uint32_t)sc[ii][1], row_top - (uint32_t)sc[ii][2], row_top - (uint32_t)sc[ii][3]};
+                    word[ii] = four_indices(away, c_int, factor, entry, sum);
+                }
+                *place(s) = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+            }
+            if (mine) atomicAdd(&row_sum[n], sum);
         }
         lds_barrier();
         // tables of the rows: a wave fills row after row
@@ -206,26 +241,35 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
 
 } // namespace
 
-// LDS for the scores of a workgroup
-static constexpr int HELD_BYTES = 128 * 1024;
+// LDS for the scores of a workgroup: all of them, or those of as many steps as leave room for the indices of the others
+static constexpr int HELD_BYTES = 136 * 1024;
 
 static int most_steps(const AttendParams &p) { return (p.c.capacity + 63) / 64; }
-static int held_bytes(const AttendParams &p) { return most_steps(p) * 4 * 64 * (p.rows < 16 ? p.rows : 16); }
+static int step_rows(const AttendParams &p) { return 4 * (p.rows < 16 ? p.rows : 16); }
+static int held_steps(const AttendParams &p)
+{
+    const int more = HELD_BYTES / (16 * step_rows(p)) - most_steps(p); // 48 bytes more for each that is held
+    return more < 0 ? -1 : std::min(most_steps(p), more / 3);
+}
+static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_steps(p) + 3 * held_steps(p)); }
 
-// Whether the keys are split over workgroups: where the scores do not fit LDS, or where a model of both times, in us, says so.  One
+// Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
 // launch takes 8 and a little for each step of the longest sequence in its workgroup, or for all bytes through the chip; three take 26
-// and what all bytes need (d 128, four rows a KV head, one launch against three with the gaps between them; 8 KV heads: 1 x 2048 keys 18.8 and
-// 24.5, 1 x 4096 36 and 26, 8 x 2048 24.7 and 29, 8 x 4096 40.4 and 34, 16 x 4096 42.5 and 46, 32 x 8192 104 and 139).
+// and what all bytes need (d 128, four rows a KV head, 8 KV heads, one launch against the sum of three: 1 x 700 keys 10.0 and 18,
+// 1 x 2048 19.3 and 18.3, 8 x 4096 41 and 30, 16 x 4096 42 and 49, 16 x 8192 78 and 86, 32 x 8192 105 and 141; eight rows, 32 x 6000
+// keys 91 and 135).
 static bool split_serves(const AttendParams &p, int d)
 {
-    if (held_bytes(p) > HELD_BYTES) return true;
+    if (held_steps(p) < 0) return true;
     const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv, size = d / 128.0;
     const double one = 8.0 + std::max(0.55 * steps * size, 0.0031 * all * size) * p.blocks, three = 26.0 + 0.0035 * all * size;
     return three < one;
 }
 
-template <int D, bool WHOLE> static void launch_waves(const AttendParams &p, void *stream)
+template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, void *stream)
 {
+    AttendParams p = p_;
+    p.held_steps = held_steps(p);
     const int waves = most_steps(p) <= 4 ? 4 : 8;
     const bool pipe = most_steps(p) > 32; // two steps in flight: 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1
     void (*kernel)(const AttendParams) = waves == 4 ? attend_kernel<D, 4, WHOLE, false> : pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;

@@ -154,7 +154,10 @@ __global__ __launch_bounds__(SNT) void cache_lookup_kernel(const AttendParams p)
         int sum = 0;
         uint32_t word[4];
 #pragma unroll
-        for (int ii = 0; ii < 4; ++ii) word[ii] = four_indices(x[ii], top, c_int, factor, entry, sum);
+        for (int ii = 0; ii < 4; ++ii) {
+            const uint32_t t = (uint32_t)top, away[4] = {t - (uint32_t)x[ii].x, t - (uint32_t)x[ii].y, t - (uint32_t)x[ii].z, t - (uint32_t)x[ii].w};
+            word[ii] = four_indices(away, c_int, factor, entry, sum);
+        }
         from[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
         atomicAdd(&total[r], sum);
     }

@@ -87,6 +87,7 @@ struct AttendParams {
     int32_t top;
     double clip, sqrt_d;
     uint32_t lut[16];
+    int32_t held_steps;        // one launch: steps of 64 keys whose scores LDS holds
     // keys split over workgroups (attend_split.hip): steps of a sequence of capacity slots, and for each launch the steps of a
     // workgroup and the workgroups of a sequence.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks of that
     // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], parameters [group][rows]; a

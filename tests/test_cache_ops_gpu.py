@@ -278,6 +278,18 @@ def test_forward_of_long_sequences(torch, ia, rows, d, page, n):
     check_forward(torch, c, got, wt, want, w, rows, "int8")
 
 
+@pytest.mark.parametrize("rows, d, page, lens", [(16, 64, 16, [2900, 0, 2112, 2113, 64]), (13, 128, 24, [2600, 2560, 1]), (9, 64, 64, [4800, 3840, 3000])])
+def test_forward_of_long_sequences_among_many_short_ones(torch, ia, rows, d, page, lens):
+    """Enough sequences for a workgroup each, and a few of them with more scores than it holds."""
+    c = Case(torch, rows, 176, 1, d, page, lens + [3] * (176 - len(lens)), room=0)
+    got, wt, want, w = run_forward(torch, ia, c, rows, 1, None)
+    check_forward(torch, c, got, wt, want, w, rows, "int8")
+    c.table[:len(lens), 1::3] = -1
+    c.up(torch)
+    got, wt, want, w = run_forward(torch, ia, c, rows, 1, None, weight=False)
+    check_forward(torch, c, got, wt, want, w, rows, "int8")
+
+
 @pytest.mark.parametrize("bits, clip", [(1, 6.6), (3, 5.5), (6, 7.7)])
 def test_forward_with_other_tables(torch, bits, clip):
     from paper_2511_21513_amd import binding
