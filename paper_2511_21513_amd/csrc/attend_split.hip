@@ -13,7 +13,6 @@
 
 #include <algorithm>
 
-
 namespace intattn {
 
 namespace {
@@ -166,9 +165,10 @@ __global__ __launch_bounds__(SNT) void cache_lookup_kernel(const AttendParams p)
         p.part_sum[((int64_t)g * p.lookup_chunks + chunk) * p.rows + row0 + i] = most[i] == HIDDEN || !rowp[i].limit ? 0 : total[i];
 }
 
-// P_hat and E / S of each index for 16 rows from row0 on; S = 0: zeros
+// P_hat and E / S of each index for 16 rows from row0 on, by the first 256 threads; S = 0: zeros
 __device__ __forceinline__ void row_tables(const AttendParams &p, int g, int steps, int row0, uint8_t (*prob)[PROB], float (*share)[64])
 {
+    if (threadIdx.x >= 256) return;
     const int live = (steps + p.lookup_steps - 1) / p.lookup_steps;
     const int r = threadIdx.x >> 4, part = threadIdx.x & 15, row = row0 + r;
     int sum = 0;
@@ -187,12 +187,12 @@ __device__ __forceinline__ void row_tables(const AttendParams &p, int g, int ste
     }
 }
 
-template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void cache_values_kernel(const AttendParams p)
+template <int D, int NW, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(64 * NW) void cache_values_kernel(const AttendParams p)
 {
     constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1;
     __shared__ uint8_t prob[16][PROB];
     __shared__ float share[WEIGHT ? 16 : 1][64];
-    __shared__ int4 widx[WEIGHT ? SWAVES : 1][64];
+    __shared__ int4 widx[WEIGHT ? NW : 1][64];
     __shared__ int acc_sum[16 * ACC_ROW];
     __shared__ int last;
     const int chunk = blockIdx.x, g = blockIdx.y, blk = blockIdx.z;
@@ -222,15 +222,15 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
     };
     const int first = s0 + wave;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + i * SWAVES, lane);
+    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + i * NW, lane);
     if (first < s1) {
         request(first, 0);
-        if (first + SWAVES < s1) request(first + SWAVES, 1);
+        if (first + NW < s1) request(first + NW, 1);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + (2 + i) * SWAVES, lane);
+    for (int i = 0; i < 2; ++i) at[i] = keys.find_v(first + (2 + i) * NW, lane);
     row_tables(p, g, gr.steps, blk * 16, prob, WEIGHT ? share : nullptr);
-    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += SNT) acc_sum[i] = 0;
+    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += 64 * NW) acc_sum[i] = 0;
     lds_barrier();
     v4i acc[CT];
 #pragma unroll
@@ -251,15 +251,15 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
             if (s * 64 + lane < gr.len) weight_out[s * 64 + lane] = p.decay * of.old + drawn;
         }
     };
-    for (int s = first; s < s1; s += 2 * SWAVES) {
+    for (int s = first; s < s1; s += 2 * NW) {
         if (s != first) {
             request(s, 0);
-            if (s + SWAVES < s1) request(s + SWAVES, 1);
+            if (s + NW < s1) request(s + NW, 1);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) at[i] = keys.find_v(s + (2 + i) * SWAVES, lane);
+            for (int i = 0; i < 2; ++i) at[i] = keys.find_v(s + (2 + i) * NW, lane);
         }
         take(s, st[0]);
-        if (s + SWAVES < s1) take(s + SWAVES, st[1]);
+        if (s + NW < s1) take(s + NW, st[1]);
     }
     if (mine) {
 #pragma unroll
@@ -272,7 +272,7 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
     constexpr int PART = 16 * D / 2; // pairs of accumulators of a chunk
     if (live > 1) {
         // device-scope stores and loads for what another workgroup reads: they pass the L2 of the XCD
-        for (int i = threadIdx.x; i < rows * D / 2; i += SNT) {
+        for (int i = threadIdx.x; i < rows * D / 2; i += 64 * NW) {
             const int *a = &acc_sum[2 * i / D * ACC_ROW + 2 * i % D];
             __hip_atomic_store(part + (int64_t)chunk * PART + i, (uint64_t)(uint32_t)a[0] | ((uint64_t)(uint32_t)a[1] << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
@@ -282,7 +282,7 @@ template <int D, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(SNT) void
         __syncthreads();
         if (last != live - 1) return;
     }
-    for (int i = threadIdx.x; i < rows * D / 2; i += SNT) {
+    for (int i = threadIdx.x; i < rows * D / 2; i += 64 * NW) {
         const int r = 2 * i / D, ch = 2 * i % D, out = blk * 16 + r;
         int sum[2] = {acc_sum[r * ACC_ROW + ch], acc_sum[r * ACC_ROW + ch + 1]};
         if (live > 1) {
@@ -373,6 +373,18 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
     return 4 * at;
 }
 
+// Waves of a workgroup of the third launch: eight where they are no more than CUs, so that each has its keys on their way at once (four
+// rows, d 128, 8 KV heads, us with four waves and with eight: 1 x 30011 keys 18.3, 16.4; 1 x 100000 36.5, 31.5; 2 x 8000 13.8, 13.0; in
+// more workgroups, 4 x 4000 .. 12400, 19.0, 25.9).
+template <int D, bool WHOLE> static void launch_values(const AttendParams &p, bool weight, hipStream_t st)
+{
+    const dim3 grid((uint32_t)p.chunks, (uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks);
+    const bool eight = (int64_t)p.chunks * p.c.B * p.c.Hkv * p.blocks <= 256;
+    void (*kernel)(const AttendParams) = eight ? (weight ? cache_values_kernel<D, 8, WHOLE, true> : cache_values_kernel<D, 8, WHOLE, false>)
+                                               : (weight ? cache_values_kernel<D, 4, WHOLE, true> : cache_values_kernel<D, 4, WHOLE, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(eight ? 512 : 256), 0, st, p);
+}
+
 template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, hipStream_t st)
 {
     const uint32_t groups = (uint32_t)(p.c.B * p.c.Hkv), supers = (uint32_t)((p.rows + SROWS - 1) / SROWS);
@@ -380,8 +392,7 @@ template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, h
     else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.score_chunks, groups, supers), dim3(SNT), 0, st, p);
     hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.lookup_chunks, groups, supers), dim3(SNT), 0, st, p);
     const bool inside = p.weight && p.blocks == 1;
-    hipLaunchKernelGGL((inside ? cache_values_kernel<D, WHOLE, true> : cache_values_kernel<D, WHOLE, false>), dim3((uint32_t)p.chunks, groups, (uint32_t)p.blocks),
-                       dim3(SNT), 0, st, p);
+    launch_values<D, WHOLE>(p, inside, st);
     if (p.weight && !inside) hipLaunchKernelGGL(cache_weights_kernel, dim3((uint32_t)((p.c.capacity + SNT - 1) / SNT), groups), dim3(SNT), 0, st, p);
 }
 
