@@ -13,14 +13,14 @@ constexpr int ANT = 256;
 constexpr int TOKENS = 4; // of a workgroup at most
 constexpr int HEAD_BYTES = 32;
 
-// Integers of x: rint of the IEEE fp32 quotient x / s, ties to even, clamped to +-127.  With r the reciprocal of s to one unit in the last place, y = fma(x, r, 128) is off
-// the quotient + 128 by less than 2^-15 where that lies in a byte's range, so wherever y is farther than 2^-14 from every half-integer
-// both round alike (units with an element nearer than that take the division), and the conversion to an unsigned byte rounds to nearest
-// even and saturates: six operations an element.
+// Integers of x: rint of the IEEE fp32 quotient x / s, ties to even, clamped to +-127.  With r the reciprocal of s to one unit in the
+// last place, y = fma(x, r, 128) is off the quotient + 128 by less than 2^-15 where that lies in a byte's range, so wherever y is farther
+// than 2^-14 from every half-integer both round alike, and the conversion to an unsigned byte rounds to nearest even and saturates: six
+// operations an element.  Units with an element nearer than that take the division, and scales whose reciprocal is no normal number.
 template <int N> __device__ __forceinline__ void quantize(const float (&x)[N], float s, uint32_t (&w)[N / 4])
 {
     const float r = __builtin_amdgcn_rcpf(s);
-    float y[N], off = 0.0f;
+    float y[N], off = s >= 0x1p-100f && s <= 0x1p100f ? 0.0f : 1.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         y[i] = __builtin_fmaf(x[i], r, 128.0f);

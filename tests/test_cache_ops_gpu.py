@@ -416,6 +416,28 @@ def test_append_leaves_absent_pages_alone_and_stays_inside_the_table(torch, ia):
     assert int((c.t["k"].cpu().numpy() != k_want).sum()) == 0
 
 
+@pytest.mark.parametrize("scale", [1e-45, 3e-41, 2.0 ** -126, 2.0 ** -101, 1e-30, 2.0 ** 101, 1e38, 3.4e38])
+def test_append_at_scales_of_all_sizes(torch, ia, scale):
+    """Subnormal scales, scales whose reciprocal is subnormal, and elements on and beside the ties."""
+    c = Case(torch, 72, 1, 2, 64, 16, [33], room=0)
+    s = np.float32(scale)
+    c.sk[:], c.sv[:] = s, s
+    c.up(torch)
+    ratio = c.rng.integers(-260, 261, (1, 2, 33, 64)) / 2.0
+    with np.errstate(over="ignore"):
+        x = (ratio * np.float64(s)).astype(np.float32)
+    x = np.where(np.isfinite(x), x, np.float32(3.4e38) * np.sign(ratio).astype(np.float32)).astype(np.float32)
+    near = c.rng.random(x.shape)
+    x = np.where(near < 0.2, np.nextafter(x, np.float32(0)), x).astype(np.float32)
+    ia.cache_append(c.cache, dev(torch, x), dev(torch, -x))
+    torch.cuda.synchronize()
+    k, v = c.t["k"].cpu().numpy(), c.t["v"].cpu().numpy()
+    for h in range(2):
+        for t in range(33):
+            page, at = c.table[0, t // 16], t % 16
+            assert (k[page, h, at] == plain.int8(x[0, h, t], s)).all() and (v[page, h, at] == plain.int8(-x[0, h, t], s)).all()
+
+
 def test_append_is_rope_and_the_quantizer(torch, ia):
     """The same integers as the library's separate operators give: rope in 32 bits, then a scale for each token."""
     xs, pos, freq, axis = rope_case(8, 2, 21, (4, 2), 64, 64, 2, 8000)
