@@ -283,7 +283,7 @@ typedef struct {
 
 /* Rotary positions on one or two tensors [B, H[i], L, d] with the same positions (Q and K of a layer).  dst may be
  * src with the same strides, else the tensors must not overlap.  src, dst and their BYTE strides (B, H, L) are
- * multiples of 16, the L strides of src at least a row; d is a multiple of 16, at most 1024. */
+ * multiples of 16, the L strides of dst at least a row; d is a multiple of 16, at most 1024; B * L < 2^24. */
 typedef struct {
     int32_t B, L, d;
     int32_t dtype;             /* 0 = fp32, 1 = fp16, 2 = bf16 */
@@ -305,7 +305,8 @@ INTATTN_API int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *args, vo
  * of its L are padding: nothing is written for their K and V, their integers and scales of Q are 0.  Inputs must be finite.
  */
 typedef struct {
-    int32_t L, Hq;             /* tokens of a sequence, 1 .. 131071; query heads, a multiple of Hkv, or 0; Hq + 2 Hkv <= 2048 */
+    int32_t L, Hq;             /* tokens of a sequence, 1 .. 131071, B * L < 2^24; query heads, a multiple of Hkv, or 0;
+                                  Hq + 2 Hkv <= 2048                                                          */
     int32_t dtype;             /* of q, k, v: 0 = fp32, 1 = fp16, 2 = bf16                                   */
     int32_t reserved;          /* must be 0                                                                  */
     const void *q, *k, *v;     /* [B, H, L, d], BYTE strides of B, H, L, all multiples of 16; q NULL if Hq = 0 */
@@ -331,7 +332,7 @@ INTATTN_API int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cach
  * comes out as zeros.  scale_q has a value for each token and head.  The output is INT8 as from intattn_forward, or
  * P_hat . V_hat s_V / 255 in floating point.  With weight, each slot j < lens[b] of each KV head gets
  *   weight_out = decay * weight + sum over the rows of its query heads and tokens of E_hat / rowSum(E_hat)
- * in fp32 (slots behind stay as they are).
+ * in fp32 (slots behind stay as they are).  out must not alias the inputs.
  */
 typedef struct {
     int32_t Hq, L;             /* query heads, a multiple of Hkv; query tokens of a sequence; Hq / Hkv * L <= 4096 */

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int64_t MOST_SLOTS = 1ll << 30; // of a sequence
 constexpr int32_t MOST_KEYS = 131071;     // of a row whose integer sums stay in 32 bits
+constexpr int64_t MOST_TOKENS = (1 << 24) - 1; // of a call: up to a workgroup of 256 threads each, and a grid's threads number below 2^32
 
 bool strides_ok(const int64_t *st, int n, int64_t multiple)
 {
@@ -239,7 +240,7 @@ int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *a, void *hip_stream)
         if (a->d < 16 || a->d % 16 != 0 || a->d > 1024) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "d must be a multiple of 16, at most 1024");
         if (a->dtype < 0 || a->dtype > 2) return fail(ctx, INTATTN_ERR_INVALID_ARG, "dtype must be 0 (fp32), 1 (fp16) or 2 (bf16)");
         if ((int64_t)a->H[0] + a->H[1] > 65535) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "more than 65535 heads");
-        if ((int64_t)a->B * a->L > 2147483647LL) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "B * L must not exceed 2^31-1");
+        if ((int64_t)a->B * a->L > MOST_TOKENS) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "B * L must not exceed 2^24-1");
         RopeParams p;
         std::memset(&p, 0, sizeof(p));
         rc = check_rotary(ctx, a->rotary, a->d, false, &p.r);
@@ -283,7 +284,7 @@ int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cache, const int
         if (a->L > MOST_KEYS) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "L must not exceed 131071");
         if (a->Hq % cache->Hkv != 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "Hq must be a multiple of Hkv");
         if ((int64_t)a->Hq + 2 * (int64_t)cache->Hkv > 2048) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "Hq + 2 Hkv must not exceed 2048");
-        if ((int64_t)cache->B * a->L > 2147483647LL) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "B * L must not exceed 2^31-1");
+        if ((int64_t)cache->B * a->L > MOST_TOKENS) return fail(ctx, INTATTN_ERR_UNSUPPORTED, "B * L must not exceed 2^24-1");
         if (a->dtype < 0 || a->dtype > 2) return fail(ctx, INTATTN_ERR_INVALID_ARG, "dtype must be 0 (fp32), 1 (fp16) or 2 (bf16)");
         if (a->reserved != 0) return fail(ctx, INTATTN_ERR_INVALID_ARG, "reserved must be 0");
         if (!a->k || !a->v) return fail(ctx, INTATTN_ERR_INVALID_ARG, "k and v must be non-NULL");

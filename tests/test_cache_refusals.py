@@ -163,6 +163,17 @@ def test_appends_that_are_refused(ia, want, kw):
     assert rc == want and text and "host-only" not in text, (rc, text)
 
 
+def test_calls_of_more_tokens_than_a_grid_has_workgroups(ia):
+    """2^24 workgroups of 256 threads are 2^32 threads."""
+    for B, L, want in ((4096, 4096, NOT), (4095, 4096, None), (1, 131071, None), (65535, 256, None), (65535, 257, NOT)):
+        a = append(L=L)
+        rc, text = code(ia, "intattn_cache_append", cache(B=B, Hkv=1), a, None)
+        assert (rc == want and "2^24" in text) if want else "host-only" in text, (B, L, rc, text)
+    for L, want in ((1 << 23, NOT), ((1 << 23) - 1, None)):
+        rc, text = code(ia, "intattn_rope", rope(L=L), None)
+        assert (rc == want and "2^24" in text) if want else "host-only" in text, (L, rc, text)
+
+
 def test_appends_without_queries_or_rotation_pass(ia):
     rc, text = code(ia, "intattn_cache_append", cache(), append(Hq=0, q=None, q_out=None, q_scale=None, rot=dict(rot=0, pos=None, freq=None)), None)
     assert "host-only" in text
