@@ -280,6 +280,18 @@ def _rows(t, what, dtype, shape, device):
     return st
 
 
+def _like(t, dtype):
+    """A new tensor in the memory order of a [B, H, L, d] tensor, where its rows can be written in pieces of 16 bytes, and its strides."""
+    import torch
+
+    out = torch.empty_like(t, dtype=dtype)
+    st = out.stride()
+    if st[3] == 1 and not (st[0] | st[1] | st[2]) & 15:
+        return out, st
+    out = torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)  # (a broadcast axis of t may end up innermost)
+    return out, out.stride()
+
+
 def _slots(t, what, dtype, B, Hkv, slots, device):
     """[B, Hkv, slots] planes (or None): the last axis is contiguous and holds every slot the call may touch."""
     if t is None:
@@ -612,8 +624,8 @@ class IntAttn:
 
         one = torch.is_tensor(x)
         xs = (x,) if one else x
-        outs = [torch.empty_like(t) for t in xs] if out is None else [out] if torch.is_tensor(out) else list(out)
-        if not 1 <= len(xs) <= 2 or len(outs) != len(xs):
+        outs = None if out is None else [out] if torch.is_tensor(out) else list(out)
+        if not 1 <= len(xs) <= 2 or (outs is not None and len(outs) != len(xs)):
             raise ValueError("one tensor or two, and as many outputs")
         a, b = xs[0], xs[-1]
         B, H, L, d = a.shape
@@ -623,8 +635,12 @@ class IntAttn:
             raise ValueError("expected float32/float16/bfloat16 tensors")
         s0, s1, s2, _ = _rows(a, "x", dtype, a.shape, dev)
         t0, t1, t2, _ = _rows(b, "x", dtype, (B, H2, L, d), dev)
-        o0, o1, o2, _ = _rows(outs[0], "out", dtype, a.shape, dev)
-        p0, p1, p2, _ = _rows(outs[-1], "out", dtype, b.shape, dev)
+        if outs is None:
+            new = [_like(t, dtype) for t in xs]
+            outs, (o0, o1, o2, _), (p0, p1, p2, _) = [n[0] for n in new], new[0][1], new[-1][1]
+        else:
+            o0, o1, o2, _ = _rows(outs[0], "out", dtype, a.shape, dev)
+            p0, p1, p2, _ = _rows(outs[-1], "out", dtype, b.shape, dev)
         args = _ROPE.pack(B, L, d, code, H, 0 if len(xs) == 1 else H2, a.data_ptr(), b.data_ptr(), outs[0].data_ptr(), outs[-1].data_ptr(),
                           s0 * es, s1 * es, s2 * es, t0 * es, t1 * es, t2 * es, o0 * es, o1 * es, o2 * es, p0 * es, p1 * es, p2 * es,
                           *_rotation(B, L, dev, pos, freq, axis, pairing, inverse))
@@ -651,11 +667,13 @@ class IntAttn:
             Hq = q.shape[1]
             q0, q1, q2, _ = _rows(q, "q", dtype, (B, Hq, L, d), dev)
             if q_out is None:
-                q_out = torch.empty((B, Hq, L, d), dtype=torch.int8, device=q.device)
+                q_out, (o0, o1, o2, _) = _like(q, torch.int8)
+            else:
+                o0, o1, o2, _ = _rows(q_out, "q_out", torch.int8, (B, Hq, L, d), dev)
             if q_scale is None:
-                q_scale = torch.empty((B, Hq, L), dtype=torch.float32, device=q.device)
-            o0, o1, o2, _ = _rows(q_out, "q_out", torch.int8, (B, Hq, L, d), dev)
-            _check(q_scale, "q_scale", torch.float32, (B, Hq, L), dev, True)
+                q_scale = q.new_empty((B, Hq, L), dtype=torch.float32)
+            else:
+                _check(q_scale, "q_scale", torch.float32, (B, Hq, L), dev, True)
         planes = (0, 0, 0, 0, 0, 0, 0)
         if weight is not None or order is not None:
             _check(first, "first", torch.int32, (B,), dev, True)
@@ -670,7 +688,8 @@ class IntAttn:
     def cache_forward(self, cache: PagedCache, q, scale_q, *, out=None, dtype=None, scale_out=None, n_new=None, max_len=0,
                       weight=None, weight_out=None, decay=1.0, stream=None):
         """intattn_cache_forward: INT8 queries [B, Hq, L, d] of the newest tokens, with a scale for each token and head, over the
-        cache.  Returns ``out`` (given, or new in ``dtype``; the default is torch.bfloat16, torch.int8 is the requantized form).  ``weight``
+        cache.  Returns ``out`` (given, or new in ``dtype`` and q's memory order; the default is torch.bfloat16, torch.int8 is the
+        requantized form).  ``weight``
         [B, Hkv, slots] float32: accumulated attention weight of each key, written to ``weight_out`` (default: in place)."""
         import torch
 
@@ -679,12 +698,15 @@ class IntAttn:
         q0, q1, q2, _ = _rows(q, "q", torch.int8, shape, dev)
         _check(scale_q, "scale_q", torch.float32, (B, Hq, L), dev, True)
         _check(n_new, "n_new", torch.int32, (B,), dev, True)
-        if out is None:
-            out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=q.device)
-        code = 3 if out.dtype is torch.int8 else _float_types().get(out.dtype)
+        if dtype is None:
+            dtype = torch.bfloat16 if out is None else out.dtype
+        code = 3 if dtype is torch.int8 else _float_types().get(dtype)
         if code is None:
             raise ValueError("out must be float32/float16/bfloat16/int8")
-        o0, o1, o2, _ = _rows(out, "out", out.dtype, shape, dev)
+        if out is None:
+            out, (o0, o1, o2, _) = _like(q, dtype)
+        else:
+            o0, o1, o2, _ = _rows(out, "out", dtype, shape, dev)
         es = out.element_size()
         per_head = int(scale_out is not None and scale_out.numel() > 1)
         _check(scale_out, "scale_out", torch.float32, (Hq if per_head else 1,), dev, True)
@@ -692,8 +714,8 @@ class IntAttn:
         if weight is not None:
             slots = min(cache.capacity, max_len) if max_len else cache.capacity
             weight_out = weight if weight_out is None else weight_out
-            planes = (weight.data_ptr(), weight_out.data_ptr(), *_slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev),
-                      *_slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev))
+            w = _slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev)
+            planes = (weight.data_ptr(), weight_out.data_ptr(), *w, *(w if weight_out is weight else _slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev)))
         args = _CACHE_FORWARD.pack(Hq, L, int(max_len), code, q.data_ptr(), q0, q1, q2, scale_q.data_ptr(), _ptr(n_new), out.data_ptr(),
                                    o0 * es, o1 * es, o2 * es, _ptr(scale_out), *planes, float(decay), per_head)
         self._done(self._lib.intattn_cache_forward(self._ctx, cache._ref, args, self._stream(dev, stream)))
@@ -713,10 +735,11 @@ class IntAttn:
         lens_out = cache.lens if lens_out is None else lens_out
         _check(total, "total", torch.int32, (B,), dev, True)
         _check(lens_out, "lens_out", torch.int32, (B,), dev, True)
+        w, o = _slots(weight, "weight", torch.float32, B, Hkv, slots, dev), _slots(order, "order", torch.int32, B, Hkv, slots, dev)
+        planes = (*w, *(w if weight_out is weight else _slots(weight_out, "weight_out", torch.float32, B, Hkv, slots, dev)),
+                  *o, *(o if order_out is order else _slots(order_out, "order_out", torch.int32, B, Hkv, slots, dev)))
         args = _EVICT.pack(int(keep), int(sink), int(recent), int(max_len), _ptr(weight), _ptr(weight_out), _ptr(order), _ptr(order_out),
-                           *_slots(weight, "weight", torch.float32, B, Hkv, slots, dev), *_slots(weight_out, "weight_out", torch.float32, B, Hkv, slots, dev),
-                           *_slots(order, "order", torch.int32, B, Hkv, slots, dev), *_slots(order_out, "order_out", torch.int32, B, Hkv, slots, dev),
-                           _ptr(total), lens_out.data_ptr())
+                           *planes, _ptr(total), lens_out.data_ptr())
         self._done(self._lib.intattn_cache_evict(self._ctx, cache._ref, args, self._stream(dev, stream)))
 
     def cache_reserve(self, cache: PagedCache, rows: int = 0, keep: int = 0, max_len: int = 0):

@@ -416,6 +416,24 @@ def test_append_leaves_absent_pages_alone_and_stays_inside_the_table(torch, ia):
     assert int((c.t["k"].cpu().numpy() != k_want).sum()) == 0
 
 
+def test_new_outputs_of_broadcast_inputs(torch, ia):
+    """Inputs with axes of stride 0, and with axes of one element of any stride."""
+    c = Case(torch, 73, 2, 2, 64, 16, [40, 33])
+    x = torch.randn((1, 1, 1, 64), device="cuda", dtype=torch.bfloat16)
+    pos, freq = torch.arange(3, device="cuda", dtype=torch.int32).expand(1, 2, 3), torch.rand(32, device="cuda", dtype=torch.float64)
+    whole = lambda t: t.contiguous()
+    for q in (x.expand(2, 4, 3, 64), x.expand(2, 4, 1, 64).contiguous().expand(2, 4, 3, 64), torch.randn((2, 3, 4, 64), device="cuda", dtype=torch.bfloat16).transpose(1, 2)):
+        assert torch.equal(ia.rope(q, pos, freq), ia.rope(whole(q), pos, freq))
+        k = q[:, :2]
+        (a, sa), (b, sb) = ia.cache_append(c.cache, k, k, q), ia.cache_append(c.cache, whole(k), whole(k), whole(q))
+        assert torch.equal(a, b) and torch.equal(sa, sb)
+        q8 = a[:1, :, :1].expand(2, 4, 3, 64)
+        assert torch.equal(ia.cache_forward(c.cache, q8, sa), ia.cache_forward(c.cache, whole(q8), sa))
+    one = torch.randn((2 * 4 * 64 + 8,), device="cuda", dtype=torch.bfloat16).as_strided((2, 4, 1, 64), (256, 64, 8, 1))
+    (a, sa), (b, sb) = ia.cache_append(c.cache, one[:, :2], one[:, :2], one), ia.cache_append(c.cache, whole(one[:, :2]), whole(one[:, :2]), whole(one))
+    assert torch.equal(a, b) and torch.equal(sa, sb)
+
+
 @pytest.mark.parametrize("scale", [1e-45, 3e-41, 2.0 ** -126, 2.0 ** -101, 1e-30, 2.0 ** 101, 1e38, 3.4e38])
 def test_append_at_scales_of_all_sizes(torch, ia, scale):
     """Subnormal scales, scales whose reciprocal is subnormal, and elements on and beside the ties."""
