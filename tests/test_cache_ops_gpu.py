@@ -482,6 +482,9 @@ EVICTS = [
     (2, 2, 64, 16, [130, 200], 100, 3, 9, "slots"),         # no orders: the slot counts
     (1, 2, 64, 32, [5000], 4999, 1, 1, "equal"),
     (1, 1, 64, 16, [20000], 9000, 4, 500, "plain"),
+    (1, 2, 64, 16, [900], 450, 0, 0, "wide"),               # weights of all exponents
+    (2, 1, 64, 16, [1300, 700], 600, 0, 0, "narrow"),       # of three values next to each other, order by order
+    (1, 2, 64, 16, [18000], 700, 3, 900, "held"),
 ]
 
 
@@ -496,6 +499,10 @@ def test_evict(torch, ia, case, place):
         w = (w * 4).astype(np.int32).astype(np.float32)
     if how == "zeros":
         w = np.where(rng.random(w.shape) < 0.7, 0, w).astype(np.float32)
+    if how == "wide":
+        w = (2.0 ** rng.uniform(-148, 127, w.shape)).astype(np.float32)
+    if how == "narrow":
+        w = (np.float32(0.3) + rng.integers(0, 3, w.shape) * np.float32(2.0 ** -25)).astype(np.float32)
     if how == "odd":
         odd = np.array([np.inf, -np.inf, np.nan, -np.nan, 0.0, -0.0, -1.5, 3e38, 1e-45], dtype=np.float32)
         w = np.where(rng.random(w.shape) < 0.5, odd[rng.integers(0, 9, w.shape)], w).astype(np.float32)
