@@ -10,7 +10,7 @@ namespace intattn {
 namespace {
 
 constexpr int ANT = 256;
-constexpr int TOKENS = 4; // of a workgroup at most
+constexpr int TOKENS = 64; // of a workgroup at most
 constexpr int HEAD_BYTES = 32;
 
 // Integers of x: rint of the IEEE fp32 quotient x / s, ties to even, clamped to +-127.  With r the reciprocal of s to one unit in the
@@ -176,10 +176,11 @@ int launch_append(const AppendParams &p_, int d, int dtype, void *stream)
     p.by_heads = fast_div((uint32_t)p.heads);
     p.by_L = fast_div((uint32_t)p.L);
     p.by_pairs = fast_div((uint32_t)(p.r.rot > 0 ? p.r.rot / 2 : 1));
-    // tokens of a workgroup: two to three rounds of its lanes where there are tokens enough (8192 tokens, us: d 128, 48 heads, one token 49.5, two
-    // 44.0, four 44.6, eight 47.2; d 64, 48 heads 34.6, 28.3, 25.9, 25.1); the heads of a token over several workgroups where there are few
+    // tokens of a workgroup where there are enough (8192 tokens, us: d 128, 48 heads, one token 49.5, two 44.0, four 44.6, eight 47.2; d 64,
+    // 48 heads 34.6, 28.3, 25.9, 25.1; 161 000 tokens, d 64, 3 heads, four tokens 68.1, 26 36.7); the heads of a token over several
+    // workgroups where there are few
     const int units = d / (dtype == 0 ? 8 : 16), rows = ANT / units;
-    p.tokens = all >= 1024 ? std::min(TOKENS, std::max(1, 768 / (p.heads * units))) : 1;
+    p.tokens = tokens_of(all, p.heads * units, 4, p.r.rot, TOKENS);
     const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.heads + rows - 1) / rows;
     const int64_t parts = blocks >= 512 ? 1 : std::min<int64_t>(rounds, std::max<int64_t>(1, 512 / blocks));
     p.turns_at = p.heads * HEAD_BYTES;

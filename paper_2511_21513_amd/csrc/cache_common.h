@@ -27,6 +27,17 @@ __device__ __forceinline__ Slot find_slot(const CacheParams &c, const int32_t *r
     return Slot{(uint32_t)page < (uint32_t)c.n_pages ? page : -1, slot - n * c.page_size};
 }
 
+// Tokens of a workgroup whose lanes take `items` pieces of each: up to `few` in three rounds of 256 lanes, or what fills one, with at
+// most 1024 angles, and 512 workgroups left.
+inline int tokens_of(int64_t tokens, int items, int few, int rot, int most)
+{
+    const int three = 768 / items < few ? 768 / items : few, one = 320 / items, angles = rot > 0 ? 2048 / rot : most;
+    int64_t n = three > one ? three : one;
+    n = n < angles ? n : angles;
+    n = n < tokens / 512 ? n : tokens / 512;
+    return (int)(n < 1 ? 1 : n < most ? n : most);
+}
+
 // ------------------------------------------------------------------ rows in lanes
 // A lane takes 32 bytes of a row, two runs of HALF channels: HALF u and on of either half of the row, or, where the rotation pairs
 // channel i with i + rot / 2, of either half of the rotated channels (so that a lane has both of each pair) and then of the others.

@@ -10,7 +10,7 @@ namespace intattn {
 
 namespace {
 
-constexpr int RNT = 256;
+constexpr int RNT = 256, TOKENS = 64;
 
 template <int DTYPE> __device__ __forceinline__ void store_unit(uint8_t *row, const Unit &un, const float (&x)[2 * HALF<DTYPE>])
 {
@@ -91,9 +91,9 @@ int launch_rope(const RopeParams &p_, int dtype, void *stream)
     p.by_units = fast_div((uint32_t)p.units);
     p.by_pairs = fast_div((uint32_t)(p.r.rot / 2));
     p.by_L = fast_div((uint32_t)p.L);
-    // tokens of a workgroup: one or two rounds of its lanes where there are tokens enough (8192 tokens of 40 heads, d 128, us: fp32, one 59.4, four
-    // 68.2; bf16, one 34.0, two 32.2, four 33.0); the heads of a token over several workgroups where there are few tokens
-    p.tokens = all >= 1024 && p.per_token < 512 ? 2 : 1;
+    // tokens of a workgroup where there are enough (8192 tokens of 40 heads, d 128, us: fp32, one 59.4, four 68.2; bf16, one 34.0, two 32.2,
+    // four 33.0; 128 000 tokens of 2 heads, fp32, d 64, two 97.9, 20 38.6); the heads of a token over several workgroups where there are few
+    p.tokens = tokens_of(all, p.per_token, 2, p.r.rot, TOKENS);
     const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.per_token + RNT - 1) / RNT;
     const int64_t parts = blocks >= 512 ? 1 : std::min<int64_t>(rounds, std::max<int64_t>(1, 512 / blocks));
     const size_t lds = sizeof(double2) * (size_t)p.tokens * (size_t)(p.r.rot / 2);
