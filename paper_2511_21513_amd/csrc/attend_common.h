@@ -239,22 +239,36 @@ __device__ __forceinline__ float drawn_by(const uint8_t *idx, const float (*shar
 {
     __builtin_amdgcn_wave_barrier();
     float sum = 0.0f;
+#pragma unroll 4
     for (int r = 0; r < rows; ++r) sum += share[r][idx[64 * r + lane]];
     __builtin_amdgcn_wave_barrier();
     return sum;
 }
 
-// channel ch of an output row; mult and shift (INT8) or unit of the row's parameters
-__device__ __forceinline__ void store_out(const AttendParams &p, float unit, int mult, int shift, uint8_t *at, int ch, int acc)
+// N channels of an output row from ch (a multiple of N) on; mult and shift (INT8) or unit of the row's parameters
+template <int N> __device__ __forceinline__ void store_out(const AttendParams &p, float unit, int mult, int shift, uint8_t *at, int ch, const int (&acc)[N])
 {
+    typedef uint8_t V1 __attribute__((ext_vector_type(N)));
+    typedef uint16_t V2 __attribute__((ext_vector_type(N)));
+    typedef float V4 __attribute__((ext_vector_type(N)));
     if (p.out_type == 3) {
-        at[ch] = (uint8_t)(int8_t)requant_any(acc, mult, shift);
+        V1 x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (uint8_t)(int8_t)requant_any(acc[i], mult, shift);
+        *(V1 *)(at + ch) = x;
         return;
     }
-    const float x = (float)acc * unit;
-    if (p.out_type == 0) ((float *)at)[ch] = x;
-    else if (p.out_type == 1) ((uint16_t *)at)[ch] = __builtin_bit_cast(uint16_t, (_Float16)x);
-    else ((uint16_t *)at)[ch] = __builtin_bit_cast(uint16_t, (__bf16)x);
+    V4 x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)acc[i] * unit;
+    if (p.out_type == 0) {
+        *(V4 *)(at + 4 * ch) = x;
+        return;
+    }
+    V2 y;
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = p.out_type == 1 ? __builtin_bit_cast(uint16_t, (_Float16)x[i]) : __builtin_bit_cast(uint16_t, (__bf16)x[i]);
+    *(V2 *)(at + 2 * ch) = y;
 }
 
 } // namespace

@@ -4,8 +4,9 @@
 // three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  Steps whose scores do not
 // fit have room for their indices there, and K of these is read again for them: with 32 sequences of 4000 to 12400 keys, 8 KV heads of
 // four rows and d 128, 135 us, 4.2 TB/s of the bytes that have to move (the three launches of attend_split.hip 144).  A workgroup
-// takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens at a time; its waves take every NW-th step of
-// 64 keys and meet at the maxima and at the sums.
+// takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens (with weights, which all rows add to, one
+// block of 16 rows after another: 32 rows of 2 keys, 4 sequences, 13.6 us; without 8.2); its waves take every NW-th step of 64 keys and
+// meet at the maxima and at the sums.
 #include "attend_common.h"
 
 #include <algorithm>
@@ -33,7 +34,7 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
     const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
     const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
-    const int held_rows = min(p.rows, 16);
+    const int held_rows = min(p.rows, 16), blk0 = gridDim.y > 1 ? blockIdx.y : 0, blk1 = gridDim.y > 1 ? blk0 + 1 : p.blocks;
     float *const weight_out = p.weight ? p.weight_out + b * p.wost[0] + kvh * p.wost[1] : nullptr;
     const int held_to = min(steps, p.held_steps);
     auto place = [&](int s) { // the lane's
@@ -41,12 +42,14 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
         return held + (s < held_to ? 4 * i : i + 3 * held_to * 4 * held_rows);
     };
     if (steps == 0) { // no keys: zeros
-        for (int i = threadIdx.x; i < p.rows * D; i += 64 * NW) store_out(p, 0.0f, 0, 31, out_row(p, b, kvh, i / D), i % D, 0);
+        const int none[4] = {0, 0, 0, 0};
+        const int end = blk1 * 16 < p.rows ? blk1 * 16 : p.rows;
+        for (int i = blk0 * 4 * D + threadIdx.x; i < end * D / 4; i += 64 * NW) store_out<4>(p, 0.0f, 0, 31, out_row(p, b, kvh, 4 * i / D), 4 * i % D, none);
         return;
     }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
 
-    for (int blk = 0; blk < p.blocks; ++blk) {
+    for (int blk = blk0; blk < blk1; ++blk) {
         const int row = blk * 16 + n;
         // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
         // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
@@ -175,11 +178,12 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
             if (mine) atomicAdd(&row_sum[n], sum);
         }
         lds_barrier();
-        // tables of the rows: a wave fills row after row
-        for (int r = wave; r < held_rows; r += NW) {
-            const uint32_t e = lane <= p.top && row_max[r] != HIDDEN ? entry[lane] : 0u, S = (uint32_t)max(row_sum[r], 1);
-            prob[r][lane] = (uint8_t)prob_u8(e, S, __builtin_amdgcn_rcpf((float)(2u * S)));
-            share[r][lane] = (float)e / (float)S;
+        // tables of the rows
+        for (int i = threadIdx.x; i < held_rows * (p.top + 1); i += 64 * NW) {
+            const int r = i / (p.top + 1), idx = i & p.top; // (2^b entries)
+            const uint32_t e = row_max[r] != HIDDEN ? entry[idx] : 0u, S = (uint32_t)max(row_sum[r], 1);
+            prob[r][idx] = (uint8_t)prob_u8(e, S, __builtin_amdgcn_rcpf((float)(2u * S)));
+            if (weight_out) share[r][idx] = (float)e / (float)S;
         }
         lds_barrier();
 
@@ -231,9 +235,10 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
                 for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
         }
         lds_barrier();
-        for (int i = threadIdx.x; i < held_rows * D; i += 64 * NW) {
-            const int r = i / D, ch = i % D, g = blk * 16 + r;
-            if (g < p.rows) store_out(p, rowp[r].unit, rowp[r].mult, rowp[r].shift, out_row(p, b, kvh, g), ch, acc_sum[r * ACC_ROW + ch]);
+        for (int i = threadIdx.x; i < held_rows * D / 4; i += 64 * NW) {
+            const int r = 4 * i / D, ch = 4 * i % D, g = blk * 16 + r;
+            const int *const a = &acc_sum[r * ACC_ROW + ch], four[4] = {a[0], a[1], a[2], a[3]};
+            if (g < p.rows) store_out<4>(p, rowp[r].unit, rowp[r].mult, rowp[r].shift, out_row(p, b, kvh, g), ch, four);
         }
         lds_barrier(); // before the next rows' parameters
     }
@@ -254,15 +259,17 @@ static int held_steps(const AttendParams &p)
 static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_steps(p) + 3 * held_steps(p)); }
 
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
-// launch takes 8 and a little for each step of the longest sequence in its workgroup, or for all bytes through the chip; three take 26
-// and what all bytes need (d 128, four rows a KV head, 8 KV heads, one launch against the sum of three: 1 x 700 keys 10.0 and 18,
-// 1 x 2048 19.3 and 18.3, 8 x 4096 41 and 30, 16 x 4096 42 and 49, 16 x 8192 78 and 86, 32 x 8192 105 and 141; eight rows, 32 x 6000
-// keys 91 and 135).
-static bool split_serves(const AttendParams &p, int d)
+// launch takes 8 and a little for each step of the longest sequence in its workgroup, or for all bytes through the chip (with weights
+// it takes blocks of rows one after another); three take 26 and what all bytes need, and further ones for more than one block of rows
+// (d 128, four rows a KV head, 8 KV heads, one launch against the sum of three: 1 x 700 keys 10.0 and 18, 1 x 2048 19.3 and 18.3,
+// 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; eight rows, 32 x 6000 keys 91 and 135).
+static bool split_serves(const AttendParams &p, int d, bool weight)
 {
     if (held_steps(p) < 0) return true;
     const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv, size = d / 128.0;
-    const double one = 8.0 + std::max(0.55 * steps * size, 0.0031 * all * size) * p.blocks, three = 26.0 + 0.0035 * all * size;
+    const int turns = weight ? p.blocks : 1;
+    const double one = 8.0 + 5.6 * (turns - 1) + std::max(0.55 * steps * turns, 0.0031 * all * p.blocks) * size;
+    const double three = 26.0 + (p.blocks > 1 ? weight ? 15.0 : 6.0 : 0.0) + 0.0035 * all * p.blocks * size;
     return three < one;
 }
 
@@ -270,17 +277,34 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
-    const int waves = most_steps(p) <= 4 ? 4 : 8;
+    const int parts = p.weight ? 1 : p.blocks; // (blocks of rows add to weights one after another)
+    // one wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0)
+    const int waves = most_steps(p) <= 1 && (int64_t)p.c.B * p.c.Hkv * parts > 512 ? 1 : most_steps(p) <= 4 ? 4 : 8;
     const bool pipe = most_steps(p) > 32; // two steps in flight: 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1
-    void (*kernel)(const AttendParams) = waves == 4 ? attend_kernel<D, 4, WHOLE, false> : pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv)), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p), (hipStream_t)stream, p);
+    void (*kernel)(const AttendParams);
+    if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
+    else if (waves == 4) kernel = attend_kernel<D, 4, WHOLE, false>;
+    else kernel = pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)parts), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
+                       (hipStream_t)stream, p);
 }
 
-int64_t attend_room(const AttendParams &p, int d) { return split_serves(p, d) ? attend_split_room(p, d, nullptr, nullptr) : 0; }
+int64_t attend_room(const AttendParams &p, int d) { return split_serves(p, d, p.weight) ? attend_split_room(p, d, nullptr, nullptr) : 0; }
+
+int64_t attend_room_upto(const AttendParams &p_, int d)
+{
+    AttendParams p = p_;
+    int64_t most = 0;
+    for (p.blocks = 1; p.blocks <= p_.blocks; ++p.blocks) { // (the choice differs between numbers of blocks)
+        p.rows = std::min(p_.rows, 16 * p.blocks);
+        if (split_serves(p, d, false) || split_serves(p, d, true)) most = std::max(most, attend_split_room(p, d, nullptr, nullptr));
+    }
+    return most;
+}
 
 int launch_attend(const AttendParams &p, int d, void *room, void *stream)
 {
-    if (split_serves(p, d)) return launch_attend_split(p, d, room, stream);
+    if (split_serves(p, d, p.weight)) return launch_attend_split(p, d, room, stream);
     const bool whole = whole_pages(p.c, d);
     if (d == 64) whole ? launch_waves<64, true>(p, stream) : launch_waves<64, false>(p, stream);
     else whole ? launch_waves<128, true>(p, stream) : launch_waves<128, false>(p, stream);

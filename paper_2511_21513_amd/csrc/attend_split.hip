@@ -187,7 +187,8 @@ __device__ __forceinline__ void row_tables(const AttendParams &p, int g, int ste
     }
 }
 
-template <int D, int NW, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(64 * NW) void cache_values_kernel(const AttendParams p)
+// ONE: one block of rows; the last of a KV head's workgroups to arrive adds their accumulators up.
+template <int D, int NW, bool WHOLE, bool ONE, bool WEIGHT> __global__ __launch_bounds__(64 * NW) void cache_values_kernel(const AttendParams p)
 {
     constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1;
     __shared__ uint8_t prob[16][PROB];
@@ -198,7 +199,7 @@ template <int D, int NW, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(6
     const int chunk = blockIdx.x, g = blockIdx.y, blk = blockIdx.z;
     const Group gr = group_of(p, g);
     const int s0 = chunk * p.chunk_steps, s1 = min(s0 + p.chunk_steps, gr.steps);
-    if (chunk > 0 && s0 >= s1) return;
+    if ((chunk > 0 || !ONE) && s0 >= s1) return;
     const int live = max((gr.steps + p.chunk_steps - 1) / p.chunk_steps, 1);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4, row = blk * 16 + n;
     const int rows = min(16, p.rows - blk * 16);
@@ -268,7 +269,15 @@ template <int D, int NW, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(6
             for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
     }
     __syncthreads();
-    uint64_t *const part = (uint64_t *)(p.part_acc + ((int64_t)g * p.blocks + blk) * p.chunks * 16 * D);
+    int *const parts = p.part_acc + ((int64_t)g * p.blocks + blk) * p.chunks * 16 * D;
+    if constexpr (!ONE) { // for cache_join_kernel
+        for (int i = threadIdx.x; i < rows * D / 4; i += 64 * NW) {
+            const int *const a = &acc_sum[4 * i / D * ACC_ROW + 4 * i % D];
+            *(int4 *)(parts + (int64_t)chunk * 16 * D + 4 * i) = make_int4(a[0], a[1], a[2], a[3]);
+        }
+        return;
+    }
+    uint64_t *const part = (uint64_t *)parts;
     constexpr int PART = 16 * D / 2; // pairs of accumulators of a chunk
     if (live > 1) {
         // device-scope stores and loads for what another workgroup reads: they pass the L2 of the XCD
@@ -301,9 +310,35 @@ template <int D, int NW, bool WHOLE, bool WEIGHT> __global__ __launch_bounds__(6
         }
         const RowParams ro = p.row_params[(int64_t)g * p.rows + out];
         uint8_t *const at = out_row(p, gr.b, gr.kvh, out);
-        store_out(p, ro.unit, ro.mult, ro.shift, at, ch, sum[0]);
-        store_out(p, ro.unit, ro.mult, ro.shift, at, ch + 1, sum[1]);
+        store_out<2>(p, ro.unit, ro.mult, ro.shift, at, ch, sum);
     }
+}
+
+// The rows where a KV head has more than one block of them: the accumulators of all chunks added up, four channels to a thread (the
+// last workgroup, on its own, took 41 us for 32 rows of 20006 keys, 8 sequences, 2 KV heads, d 128; apart both take 34.  For one block of
+// four rows of 30011 keys 18.4 apart, 16.7 so).
+constexpr int JNT = 64;
+template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const AttendParams p)
+{
+    const int g = blockIdx.y, i = blockIdx.x * JNT + threadIdx.x, row = 4 * i / D, ch = 4 * i % D;
+    if (row >= p.rows) return;
+    const Group gr = group_of(p, g);
+    const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
+    const int *const part = p.part_acc + ((int64_t)g * p.blocks + row / 16) * p.chunks * 16 * D + row % 16 * D + ch;
+    const RowParams ro = p.row_params[(int64_t)g * p.rows + row];
+    int sum[4] = {0, 0, 0, 0};
+    constexpr int BATCH = 16; // loads in flight
+    for (int c = 0; c < live; c += BATCH) {
+        int4 x[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) x[u] = *(const int4 *)(part + (int64_t)min(c + u, live - 1) * 16 * D);
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            if (c + u >= live) break;
+            sum[0] += x[u].x, sum[1] += x[u].y, sum[2] += x[u].z, sum[3] += x[u].w;
+        }
+    }
+    store_out<4>(p, ro.unit, ro.mult, ro.shift, out_row(p, gr.b, gr.kvh, row), ch, sum);
 }
 
 // Weights where a KV head has more than 16 rows: a thread for each key, over all rows.
@@ -324,6 +359,7 @@ __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p
         const int rows = min(16, p.rows - blk * 16);
         if (mine) {
             const uint8_t *at = (const uint8_t *)(step_of(p, g, slot >> 6) + blk * 16 * 4) + (slot & 63);
+#pragma unroll 8
             for (int r = 0; r < rows; ++r) drawn += share[r][at[64 * r]];
         }
     }
@@ -376,12 +412,14 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
 // Waves of a workgroup of the third launch: eight where they are no more than CUs, so that each has its keys on their way at once (four
 // rows, d 128, 8 KV heads, us with four waves and with eight: 1 x 30011 keys 18.3, 16.4; 1 x 100000 36.5, 31.5; 2 x 8000 13.8, 13.0; in
 // more workgroups, 4 x 4000 .. 12400, 19.0, 25.9).
-template <int D, bool WHOLE> static void launch_values(const AttendParams &p, bool weight, hipStream_t st)
+template <int D, bool WHOLE> static void launch_values(const AttendParams &p, hipStream_t st)
 {
     const dim3 grid((uint32_t)p.chunks, (uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks);
     const bool eight = (int64_t)p.chunks * p.c.B * p.c.Hkv * p.blocks <= 256;
-    void (*kernel)(const AttendParams) = eight ? (weight ? cache_values_kernel<D, 8, WHOLE, true> : cache_values_kernel<D, 8, WHOLE, false>)
-                                               : (weight ? cache_values_kernel<D, 4, WHOLE, true> : cache_values_kernel<D, 4, WHOLE, false>);
+    void (*kernel)(const AttendParams);
+    if (p.blocks > 1) kernel = eight ? cache_values_kernel<D, 8, WHOLE, false, false> : cache_values_kernel<D, 4, WHOLE, false, false>;
+    else if (p.weight) kernel = eight ? cache_values_kernel<D, 8, WHOLE, true, true> : cache_values_kernel<D, 4, WHOLE, true, true>;
+    else kernel = eight ? cache_values_kernel<D, 8, WHOLE, true, false> : cache_values_kernel<D, 4, WHOLE, true, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(eight ? 512 : 256), 0, st, p);
 }
 
@@ -391,9 +429,10 @@ template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, h
     if (p.blocks == 1) hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, true>), dim3((uint32_t)p.score_chunks, groups, 1), dim3(SNT), 0, st, p);
     else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.score_chunks, groups, supers), dim3(SNT), 0, st, p);
     hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.lookup_chunks, groups, supers), dim3(SNT), 0, st, p);
-    const bool inside = p.weight && p.blocks == 1;
-    launch_values<D, WHOLE>(p, inside, st);
-    if (p.weight && !inside) hipLaunchKernelGGL(cache_weights_kernel, dim3((uint32_t)((p.c.capacity + SNT - 1) / SNT), groups), dim3(SNT), 0, st, p);
+    launch_values<D, WHOLE>(p, st);
+    if (p.blocks == 1) return;
+    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((uint32_t)((p.rows * D / 4 + JNT - 1) / JNT), groups), dim3(JNT), 0, st, p);
+    if (p.weight) hipLaunchKernelGGL(cache_weights_kernel, dim3((uint32_t)((p.c.capacity + SNT - 1) / SNT), groups), dim3(SNT), 0, st, p);
 }
 
 int launch_attend_split(const AttendParams &p_, int d, void *room, void *stream)

@@ -384,7 +384,7 @@ int intattn_cache_reserve(intattn_ctx *ctx, const intattn_cache *cache, int32_t 
             p.c = c;
             p.rows = rows;
             p.blocks = (rows + 15) / 16;
-            bytes = std::max(bytes, attend_room(p, cache->d));
+            bytes = std::max(bytes, attend_room_upto(p, cache->d));
         }
         if (keep > 0) {
             EvictParams p;

@@ -116,6 +116,8 @@ int launch_rope(const RopeParams &p, int dtype, void *stream);
 int launch_append(const AppendParams &p, int d, int dtype, void *stream);
 // bytes of room that launch_attend needs for these parameters
 int64_t attend_room(const AttendParams &p, int d);
+// and for any with at most as many rows, with weights or without
+int64_t attend_room_upto(const AttendParams &p, int d);
 int launch_attend(const AttendParams &p, int d, void *room, void *stream);
 int64_t attend_split_room(const AttendParams &p, int d, void *room, AttendParams *out);
 int launch_attend_split(const AttendParams &p, int d, void *room, void *stream);

@@ -655,6 +655,34 @@ def test_captured_step_replays_with_new_lengths(torch):
     ia.close()
 
 
+def test_room_is_reserved_for_fewer_rows_too(torch):
+    """The kernels that a call takes depend on its rows and on whether weights are kept; a reservation holds for all of them."""
+    from paper_2511_21513_amd import binding
+
+    own = binding.IntAttn(device=0)
+    c = Case(torch, 121, 1, 2, 64, 16, [2600], room=0)
+    own.cache_reserve(c.cache, rows=40)
+    for rows, L in ((1, 1), (4, 1), (16, 1), (5, 4), (20, 2), (40, 1)):
+        for weight in (False, True):
+            q, s, qt, st = c.queries(torch, 2 * rows, L) if rows * L <= 40 else (None,) * 4
+            if q is None:
+                continue
+            w = torch.rand((1, 2, c.width * 16), device="cuda") if weight else None
+            out, stream = torch.empty((1, 2 * rows, L, 64), dtype=torch.int8, device="cuda"), torch.cuda.Stream()
+            graph = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph, stream=stream):
+                own.cache_forward(c.cache, qt, st, out=out, weight=w)
+            want = plain.attend(q, s, c.k, c.v, c.table, c.lens, c.sk, c.sv)[1]
+            for _ in range(3):
+                out.fill_(77)
+                graph.replay()
+                torch.cuda.synchronize()
+                assert int((out.cpu().numpy() != want).sum()) == 0
+            del graph
+    own.close()
+
+
 def test_a_captured_call_without_room_is_refused(torch):
     from paper_2511_21513_amd import binding
 
