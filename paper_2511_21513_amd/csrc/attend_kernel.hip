@@ -259,17 +259,19 @@ static int held_steps(const AttendParams &p)
 static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_steps(p) + 3 * held_steps(p)); }
 
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
-// launch takes 8 and a little for each step of the longest sequence in its workgroup, or for all bytes through the chip (with weights
-// it takes blocks of rows one after another); three take 26 and what all bytes need, and further ones for more than one block of rows
-// (d 128, four rows a KV head, 8 KV heads, one launch against the sum of three: 1 x 700 keys 10.0 and 18, 1 x 2048 19.3 and 18.3,
-// 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; eight rows, 32 x 6000 keys 91 and 135).
+// launch takes 8, a third or half for each step of the longest sequence in its workgroup and a little for its rows, or what all bytes
+// take through the chip; with weights it takes blocks of rows one after another.  Three take 17 and what all bytes need, and further ones
+// for more than one block of rows.  (8 KV heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15,
+// 1 x 2048 19.3 and 18.3, 8 x 1024 15 and 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; one
+// KV head of 32 rows, d 64, 32 x 1 .. 4380 keys 30 and 28.)
 static bool split_serves(const AttendParams &p, int d, bool weight)
 {
     if (held_steps(p) < 0) return true;
-    const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv, size = d / 128.0;
+    const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv * p.blocks, size = d / 128.0;
     const int turns = weight ? p.blocks : 1;
-    const double one = 8.0 + 5.6 * (turns - 1) + std::max(0.55 * steps * turns, 0.0031 * all * p.blocks) * size;
-    const double three = 26.0 + (p.blocks > 1 ? weight ? 15.0 : 6.0 : 0.0) + 0.0035 * all * p.blocks * size;
+    const double step = (steps <= 32 ? 0.35 : 0.48) * size + 0.0065 * std::min(p.rows, 16);
+    const double one = 8.0 + 5.6 * (turns - 1) + std::max(steps * turns * step, 0.0031 * all * size);
+    const double three = 17.0 + (p.blocks > 1 ? weight ? 15.0 : 6.0 : 0.0) + 0.0035 * all * size;
     return three < one;
 }
 

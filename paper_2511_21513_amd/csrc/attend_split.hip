@@ -326,6 +326,11 @@ template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const 
     const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
     const int *const part = p.part_acc + ((int64_t)g * p.blocks + row / 16) * p.chunks * 16 * D + row % 16 * D + ch;
     const RowParams ro = p.row_params[(int64_t)g * p.rows + row];
+    if (ch == 0) { // for the weights
+        int total = 0;
+        for (int c = 0; c < (gr.steps + p.lookup_steps - 1) / p.lookup_steps; ++c) total += p.part_sum[((int64_t)g * p.lookup_chunks + c) * p.rows + row];
+        p.row_sum[(int64_t)g * p.rows + row] = total;
+    }
     int sum[4] = {0, 0, 0, 0};
     constexpr int BATCH = 16; // loads in flight
     for (int c = 0; c < live; c += BATCH) {
@@ -341,25 +346,27 @@ template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const 
     store_out<4>(p, ro.unit, ro.mult, ro.shift, out_row(p, gr.b, gr.kvh, row), ch, sum);
 }
 
-// Weights where a KV head has more than 16 rows: a thread for each key, over all rows.
+// Weights where a KV head has more than 16 rows: a thread for each key, over all rows, E / S of 64 rows at a time in LDS.
 __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p)
 {
-    __shared__ uint8_t prob[16][PROB];
-    __shared__ float share[16][64];
-    const int g = blockIdx.y;
+    constexpr int AT_ONCE = 64;
+    __shared__ float share[AT_ONCE][64];
+    const int g = blockIdx.y, slot = blockIdx.x * SNT + threadIdx.x;
     const Group gr = group_of(p, g);
-    const int slot = blockIdx.x * SNT + threadIdx.x;
     if ((int)blockIdx.x * SNT >= gr.len) return;
     const bool mine = slot < gr.len;
     float drawn = 0.0f;
-    for (int blk = 0; blk < p.blocks; ++blk) {
+    for (int row0 = 0; row0 < p.rows; row0 += AT_ONCE) {
+        const int rows = min(AT_ONCE, p.rows - row0);
         __syncthreads();
-        row_tables(p, g, gr.steps, blk * 16, prob, share);
+        for (int i = threadIdx.x; i < rows * (p.top + 1); i += SNT) {
+            const int r = i / (p.top + 1), idx = i & p.top, sum = p.row_sum[(int64_t)g * p.rows + row0 + r]; // (2^b entries)
+            share[r][idx] = sum > 0 ? (float)((p.lut[idx >> 2] >> (8 * (idx & 3))) & 0xffu) / (float)sum : 0.0f;
+        }
         __syncthreads();
-        const int rows = min(16, p.rows - blk * 16);
         if (mine) {
-            const uint8_t *at = (const uint8_t *)(step_of(p, g, slot >> 6) + blk * 16 * 4) + (slot & 63);
-#pragma unroll 8
+            const uint8_t *at = (const uint8_t *)(step_of(p, g, slot >> 6) + row0 * 4) + (slot & 63);
+#pragma unroll 16
             for (int r = 0; r < rows; ++r) drawn += share[r][at[64 * r]];
         }
     }
@@ -404,6 +411,7 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
     p.part_sum = take(groups * p.lookup_chunks * p.rows);
     p.part_acc = take(groups * p.blocks * p.chunks * 16 * d);
     p.arrived = take(groups * p.blocks);
+    p.row_sum = take(groups * p.rows);
     p.row_params = (RowParams *)take(groups * p.rows * (int64_t)(sizeof(RowParams) / 4));
     if (out) *out = p;
     return 4 * at;

@@ -90,10 +90,10 @@ struct AttendParams {
     int32_t held_steps;        // one launch: steps of 64 keys whose scores LDS holds
     // keys split over workgroups (attend_split.hip): steps of a sequence of capacity slots, and for each launch the steps of a
     // workgroup and the workgroups of a sequence.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks of that
-    // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], parameters [group][rows]; a
-    // group is a (sequence, KV head)
+    // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], sums and parameters
+    // [group][rows]; a group is a (sequence, KV head)
     int32_t steps, score_steps, score_chunks, lookup_steps, lookup_chunks, chunk_steps, chunks;
-    int32_t *scores, *part_max, *part_sum, *part_acc, *arrived;
+    int32_t *scores, *part_max, *part_sum, *part_acc, *arrived, *row_sum;
     RowParams *row_params;
 };
 
