@@ -66,8 +66,8 @@ __device__ __forceinline__ void transpose4(const uint32_t w0, const uint32_t w1,
 // Where lanes find their keys.  WHOLE: pages of a multiple of 16 keys whose rows follow each other, so that 16 keys from a multiple of 16
 // on are one run of 16 d bytes: one look into the table, and offsets that are part of the instruction (with a stride that is not known
 // the sixteen addresses of a step of V took 32 registers).  Keys past the end are read where the table says, which does not wait for
-// the length, and keys of pages that are not there from the pool's first page (the probability of either is 0).  V is read once and in whole lines, past the caches (8 KiB blocks in no order: 6.1 TB/s,
-// 5.4 through them); half lines of K need the cache.
+// the length, and keys of pages that are not there from the pool's first page (the probability of either is 0).  V that is read once
+// is read in whole lines past the caches (8 KiB blocks in no order: 6.1 TB/s, 5.4 through them); half lines of K need the cache.
 //
 // find_*() asks the table, load_*() for the keys.  They are apart so that a loop can ask for the places of a step before it asks for the
 // keys of an earlier one: loads come back in order, and a place asked for last could only be waited for together with every key
@@ -114,8 +114,8 @@ template <int D, bool WHOLE> struct Keys {
             for (int j = 0; j < D / 64; ++j) a[i][j] = *(const v4i *)(from + 64 * j);
         }
     }
-    // d / 16 channels, from d / 16 m on, of the lane's 16 keys
-    __device__ __forceinline__ void load_v(const Place &p, int lane, uint32_t (&v)[16][D / 64]) const
+    // d / 16 channels, from d / 16 m on, of the lane's 16 keys; ONCE: no other workgroup reads them
+    template <bool ONCE = true> __device__ __forceinline__ void load_v(const Place &p, int lane, uint32_t (&v)[16][D / 64]) const
     {
         const bool is = there(p);
         const int page = is ? p.entry : 0, at = is ? p.at : 0;
@@ -125,11 +125,14 @@ template <int D, bool WHOLE> struct Keys {
             const int8_t *key = from + i * D;
             if constexpr (!WHOLE) key = from + __shfl(page, (lane & 48) + i) * c.vs[0] + __shfl(at, (lane & 48) + i) * c.vs[2];
             if constexpr (D == 128) {
-                const v2i w = __builtin_nontemporal_load((const v2i *)key);
+                v2i w;
+                if constexpr (ONCE) w = __builtin_nontemporal_load((const v2i *)key);
+                else w = *(const v2i *)key;
                 v[i][0] = (uint32_t)w[0];
                 v[i][1] = (uint32_t)w[1];
             } else {
-                v[i][0] = __builtin_nontemporal_load((const uint32_t *)key);
+                if constexpr (ONCE) v[i][0] = __builtin_nontemporal_load((const uint32_t *)key);
+                else v[i][0] = *(const uint32_t *)key;
             }
         }
     }

@@ -3,7 +3,8 @@
 // maxima cannot be joined afterwards, so the work is cut at both, each a launch boundary: no workgroup waits for another.
 //   scores   Q.K^T of a chunk of keys: INT32 scores to room of the context, a maximum for each row and chunk
 //   lookup   the row's maximum; scores become table indices (a byte each, in place), a sum for each row and chunk
-//   values   the row's sum; P.V of a chunk; the last workgroup of a KV head's chunks adds them up and writes the rows
+//   values   the row's sum; P.V of a chunk; the last workgroup of a KV head's chunks adds them up and writes the rows.  With more than
+//            one block of 16 rows a fourth launch does, and a fifth forms the weights.
 // K and V are read once, and the scores (4 bytes for each row and key against 2 d for a key) mostly stay in the caches between the
 // launches.  The chunks of all sequences are one grid of small workgroups, which evens out sequences of different lengths.
 //
@@ -217,7 +218,7 @@ template <int D, int NW, bool WHOLE, bool ONE, bool WEIGHT> __global__ __launch_
     typename Keys<D, WHOLE>::Place at[2];
     auto request = [&](int s, int i) {
         Step &to = st[i];
-        keys.load_v(at[i], lane, to.v);
+        keys.template load_v<ONE>(at[i], lane, to.v);
         to.x = step_of(p, g, s)[(mine ? row : blk * 16) * 4 + kb];
         if constexpr (WEIGHT) to.old = weight[min(s * 64 + lane, gr.len - 1)];
     };
@@ -315,8 +316,8 @@ template <int D, int NW, bool WHOLE, bool ONE, bool WEIGHT> __global__ __launch_
 }
 
 // The rows where a KV head has more than one block of them: the accumulators of all chunks added up, four channels to a thread (the
-// last workgroup, on its own, took 41 us for 32 rows of 20006 keys, 8 sequences, 2 KV heads, d 128; apart both take 34.  For one block of
-// four rows of 30011 keys 18.4 apart, 16.7 so).
+// last workgroup, on its own, took 41 us for 32 rows of 20006 keys, 8 sequences, 2 KV heads, d 128, apart both take 34 and with V
+// through the caches 30.  For one block of four rows of 30011 keys 18.4 apart, 16.7 so).
 constexpr int JNT = 64;
 template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const AttendParams p)
 {
@@ -326,10 +327,12 @@ template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const 
     const int live = (gr.steps + p.chunk_steps - 1) / p.chunk_steps;
     const int *const part = p.part_acc + ((int64_t)g * p.blocks + row / 16) * p.chunks * 16 * D + row % 16 * D + ch;
     const RowParams ro = p.row_params[(int64_t)g * p.rows + row];
-    if (ch == 0) { // for the weights
+    if (p.weight) { // the row's sum for the next launch, by the lanes that have the row
         int total = 0;
-        for (int c = 0; c < (gr.steps + p.lookup_steps - 1) / p.lookup_steps; ++c) total += p.part_sum[((int64_t)g * p.lookup_chunks + c) * p.rows + row];
-        p.row_sum[(int64_t)g * p.rows + row] = total;
+        for (int c = ch / 4; c < (gr.steps + p.lookup_steps - 1) / p.lookup_steps; c += D / 4) total += p.part_sum[((int64_t)g * p.lookup_chunks + c) * p.rows + row];
+#pragma unroll
+        for (int o = 1; o < D / 4; o *= 2) total += __shfl_xor(total, o);
+        if (ch == 0) p.row_sum[(int64_t)g * p.rows + row] = total;
     }
     int sum[4] = {0, 0, 0, 0};
     constexpr int BATCH = 16; // loads in flight
@@ -346,7 +349,8 @@ template <int D> __global__ __launch_bounds__(JNT) void cache_join_kernel(const 
     store_out<4>(p, ro.unit, ro.mult, ro.shift, out_row(p, gr.b, gr.kvh, row), ch, sum);
 }
 
-// Weights where a KV head has more than 16 rows: a thread for each key, over all rows, E / S of 64 rows at a time in LDS.
+// Weights where a KV head has more than 16 rows: a thread for each key, over all rows, E / S of 64 rows at a time in LDS (64
+// keys and a quarter of the rows to each wave: 7.0 -> 14.1 us for 32 rows of 20006 keys, 8 sequences, 2 KV heads, and 17.1 -> 12.9 for 224 rows).
 __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p)
 {
     constexpr int AT_ONCE = 64;
@@ -385,11 +389,12 @@ static void plan(AttendParams &p)
     // as many steps as leave `workgroups` workgroups, between `least` and what makes `most` chunks of a sequence
     auto steps_of = [&](int64_t workgroups, int64_t least, int64_t most) {
         const int64_t c = std::max(std::max((all + workgroups - 1) / workgroups, least), (p.steps + most - 1) / most);
-        return (int32_t)((c + SWAVES - 1) / SWAVES * SWAVES);
+        return (int32_t)c;
     };
-    p.score_steps = steps_of(16384, 4, 256);
-    p.lookup_steps = steps_of(1536, 8, 256);
-    p.chunk_steps = steps_of(3072, 8, 32);
+    auto whole = [](int32_t steps) { return (steps + SWAVES - 1) / SWAVES * SWAVES; };
+    p.score_steps = whole(steps_of(16384, 4, 256));
+    p.lookup_steps = steps_of(1536, p.rows <= 16 ? 8 : std::max(1, 128 / p.rows), 256);
+    p.chunk_steps = whole(steps_of(3072, 8, 32));
     p.score_chunks = (p.steps + p.score_steps - 1) / p.score_steps;
     p.lookup_chunks = (p.steps + p.lookup_steps - 1) / p.lookup_steps;
     p.chunks = (p.steps + p.chunk_steps - 1) / p.chunk_steps;
