@@ -280,12 +280,19 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
     AttendParams p = p_;
     p.held_steps = held_steps(p);
     const int parts = p.weight ? 1 : p.blocks; // (blocks of rows add to weights one after another)
-    // one wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0)
-    const int waves = most_steps(p) <= 1 && (int64_t)p.c.B * p.c.Hkv * parts > 512 ? 1 : most_steps(p) <= 4 ? 4 : 8;
-    const bool pipe = most_steps(p) > 32; // two steps in flight: 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1
+    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
+    // Four where a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their way while the other
+    // looks up indices (eight waves and four, us: 512 of 100 .. 3700 keys 87.1, 69.1; 320 of 1000 .. 3000 56.6, 48.0; 2048 of 300 ..
+    // 1000 110, 82; but 272 of 300 .. 1800 32.0, 35.4).
+    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * parts;
+    const bool two = groups >= 320 && held_bytes(p) <= 60 * 1024;
+    const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
+    // two steps in flight: 8 groups, 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1; 512 groups of four waves,
+    // 32 steps 52.6, 54.0; 57 steps 95.9, 90.3
+    const bool pipe = most_steps(p) > 32;
     void (*kernel)(const AttendParams);
     if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
-    else if (waves == 4) kernel = attend_kernel<D, 4, WHOLE, false>;
+    else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;
     else kernel = pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)parts), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
                        (hipStream_t)stream, p);
