@@ -249,7 +249,8 @@ INTATTN_API int intattn_index_softmax(intattn_ctx *ctx, const intattn_softmax_ar
  * An entry that is not in 0 .. n_pages - 1 stands for a page that is not there: its keys are hidden, and nothing is written
  * to them.  lens[b], the number of slots in use, is taken as at least 0 and at most max_pages * page_size; the caller
  * keeps it.  Sequences may share pages that none of them writes to.  Scales that are not finite and > 0 cannot be
- * reported by return code: rows that they belong to come out as zeros.  Everything in the struct but the scalars is
+ * reported by return code: rows that they belong to come out as zeros.  Outputs, pages that are written to and planes of
+ * weights or orders must not lie over themselves or each other (a stride of 0 is refused where it shows).  Everything in the struct but the scalars is
  * DEVICE memory that the kernels read when they run: a captured call sees the lengths, tables and scales of its replay.
  */
 typedef struct {
@@ -283,7 +284,7 @@ typedef struct {
 
 /* Rotary positions on one or two tensors [B, H[i], L, d] with the same positions (Q and K of a layer).  dst may be
  * src with the same strides, else the tensors must not overlap.  src, dst and their BYTE strides (B, H, L) are
- * multiples of 16, the L strides of dst at least a row; d is a multiple of 16, at most 1024; B * L < 2^24. */
+ * multiples of 16, the strides of dst at least a row; d is a multiple of 16, at most 1024; B * L < 2^24. */
 typedef struct {
     int32_t B, L, d;
     int32_t dtype;             /* 0 = fp32, 1 = fp16, 2 = bf16 */

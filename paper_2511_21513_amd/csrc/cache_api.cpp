@@ -24,6 +24,9 @@ bool strides_ok(const int64_t *st, int n, int64_t multiple)
         if (st[i] < 0 || st[i] % multiple != 0) return false;
     return true;
 }
+// what is written must not lie over itself: a stride below a row, along an axis of more than one
+bool apart(const int64_t *st, int64_t n0, int64_t n1, int64_t n2, int64_t row) { return (n0 == 1 || st[0] >= row) && (n1 == 1 || st[1] >= row) && (n2 == 1 || st[2] >= row); }
+bool apart(const int64_t *st, int64_t n0, int64_t n1) { return (n0 == 1 || st[0] >= 1) && (n1 == 1 || st[1] >= 1); }
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 int check_ctx(intattn_ctx *ctx, const void *args)
@@ -73,6 +76,8 @@ int check_cache(intattn_ctx *ctx, const intattn_cache *c, CacheParams *p)
     p->by_page = fast_div((uint32_t)c->page_size);
     return INTATTN_OK;
 }
+
+bool writable(const intattn_cache *c) { return apart(c->k_stride, c->n_pages, c->Hkv, 1, c->d) && apart(c->v_stride, c->n_pages, c->Hkv, 1, c->d); }
 
 // max_len of a call into the parameters' capacity
 int bound_len(intattn_ctx *ctx, int32_t max_len, CacheParams *p)
@@ -159,6 +164,8 @@ int forward_params(intattn_ctx *ctx, const intattn_cache *cache, const intattn_c
     if (!a->q || !a->scale_q || !a->out) return fail(ctx, INTATTN_ERR_INVALID_ARG, "q, scale_q, out must be non-NULL");
     if (!aligned(a->q, 16) || !aligned(a->out, 16) || !strides_ok(a->q_stride, 3, 16) || !strides_ok(a->out_stride, 3, 16))
         return fail(ctx, INTATTN_ERR_INVALID_ARG, "q, out and their strides must be multiples of 16");
+    if (!apart(a->out_stride, cache->B, a->Hq, a->L, (int64_t)cache->d * (a->out_type == 0 ? 4 : a->out_type == 3 ? 1 : 2)))
+        return fail(ctx, INTATTN_ERR_INVALID_ARG, "the strides of out must cover a row");
     if (!aligned(a->scale_q, 4) || !aligned(a->scale_out, 4) || !aligned(a->n_new, 4) || !aligned(a->weight, 4) || !aligned(a->weight_out, 4))
         return fail(ctx, INTATTN_ERR_INVALID_ARG, "scales, n_new and weights must be 4-byte aligned");
     if ((a->weight == nullptr) != (a->weight_out == nullptr)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "weight and weight_out go together");
@@ -167,6 +174,7 @@ int forward_params(intattn_ctx *ctx, const intattn_cache *cache, const intattn_c
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "strides of the weights must be >= 0");
         if (a->weight == a->weight_out && (a->weight_stride[0] != a->weight_out_stride[0] || a->weight_stride[1] != a->weight_out_stride[1]))
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "weight_out is weight with other strides");
+        if (!apart(a->weight_out_stride, cache->B, cache->Hkv)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "planes that are written must not lie over each other");
         if (!std::isfinite(a->decay)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "decay must be finite");
     }
     p->q = a->q; p->scale_q = a->scale_q; p->n_new = a->n_new;
@@ -200,6 +208,9 @@ int evict_params(intattn_ctx *ctx, const intattn_cache *cache, const intattn_evi
         return fail(ctx, INTATTN_ERR_INVALID_ARG, "weights, orders, total and lens_out must be 4-byte aligned");
     if (!strides_ok(a->weight_stride, 2, 1) || !strides_ok(a->weight_out_stride, 2, 1) || !strides_ok(a->order_stride, 2, 1) || !strides_ok(a->order_out_stride, 2, 1))
         return fail(ctx, INTATTN_ERR_INVALID_ARG, "strides of weights and orders must be >= 0");
+    if (!apart(a->weight_out_stride, cache->B, cache->Hkv) || (a->order && !apart(a->order_out_stride, cache->B, cache->Hkv)))
+        return fail(ctx, INTATTN_ERR_INVALID_ARG, "planes that are written must not lie over each other");
+    if (!writable(cache)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "pages and heads of a cache that is written to must not lie over each other");
     for (int i = 0; i < 2; ++i)
         if ((a->weight == a->weight_out && a->weight_stride[i] != a->weight_out_stride[i]) ||
             (a->order && a->order == a->order_out && a->order_stride[i] != a->order_out_stride[i]))
@@ -250,7 +261,7 @@ int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *a, void *hip_stream)
             if (!a->src[i] || !a->dst[i]) return fail(ctx, INTATTN_ERR_INVALID_ARG, "src and dst must be non-NULL");
             if (!aligned(a->src[i], 16) || !aligned(a->dst[i], 16) || !strides_ok(a->src_stride[i], 3, 16) || !strides_ok(a->dst_stride[i], 3, 16))
                 return fail(ctx, INTATTN_ERR_INVALID_ARG, "src, dst and their strides must be multiples of 16");
-            if (a->L > 1 && a->dst_stride[i][2] < row) return fail(ctx, INTATTN_ERR_INVALID_ARG, "the L strides of dst must cover a row");
+            if (!apart(a->dst_stride[i], a->B, a->H[i], a->L, row)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "the strides of dst must cover a row");
             if (a->src[i] == a->dst[i])
                 for (int s = 0; s < 3; ++s)
                     if (a->src_stride[i][s] != a->dst_stride[i][s]) return fail(ctx, INTATTN_ERR_INVALID_ARG, "dst is src with other strides");
@@ -296,10 +307,14 @@ int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cache, const int
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "k, v and their strides must be multiples of 16");
         if (a->Hq > 0 && (!aligned(a->q, 16) || !aligned(a->q_out, 16) || !strides_ok(a->q_stride, 3, 16) || !strides_ok(a->q_out_stride, 3, 16)))
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "q, q_out and their strides must be multiples of 16");
+        if (a->Hq > 0 && !apart(a->q_out_stride, cache->B, a->Hq, a->L, cache->d)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "the strides of q_out must cover a row");
+        if (!writable(cache)) return fail(ctx, INTATTN_ERR_INVALID_ARG, "pages and heads of a cache that is written to must not lie over each other");
         if (!aligned(a->q_scale, 4) || !aligned(a->n_new, 4) || !aligned(a->weight, 4) || !aligned(a->order, 4) || !aligned(a->first, 4))
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "q_scale, n_new, weight, order and first must be 4-byte aligned");
         if ((a->weight && !strides_ok(a->weight_stride, 2, 1)) || (a->order && !strides_ok(a->order_stride, 2, 1)))
             return fail(ctx, INTATTN_ERR_INVALID_ARG, "strides of weights and orders must be >= 0");
+        if ((a->weight && !apart(a->weight_stride, cache->B, cache->Hkv)) || (a->order && !apart(a->order_stride, cache->B, cache->Hkv)))
+            return fail(ctx, INTATTN_ERR_INVALID_ARG, "planes that are written must not lie over each other");
         const void *x[3] = {a->q, a->k, a->v};
         const int64_t *xs[3] = {a->q_stride, a->k_stride, a->v_stride};
         for (int i = 0; i < 3; ++i) {

@@ -55,6 +55,9 @@ ROPES = [
     ("float16", 2, 7, (1, 1), 256, 256, 4, False, 70000, False),
     ("float16", 1, 3, (2,), 1024, 256, 2, False, 70000, True),
     ("bfloat16", 1, 300, (33, 7), 64, 16, 2, True, 30, False),
+    ("float32", 3, 700, (1, 1), 64, 32, 1, False, 4000, False),      # many tokens to a workgroup
+    ("float16", 7, 401, (1,), 16, 16, 1, True, 4000, True),
+    ("bfloat16", 1, 5, (257, 1), 1024, 256, 4, False, 300, False),
 ]
 
 
@@ -357,6 +360,9 @@ APPENDS = [
     ("float32", 2, 0, 3, 128, 1, 5, [5, 9], None, 128, 1, True, True),
     ("float16", 1, 2, 1, 64, 7, 70, [70], [65], 0, 1, False, True),
     ("float32", 2, 40, 8, 128, 16, 3, [3, 40], [9, -2], 64, 1, False, True),
+    ("bfloat16", 1, 2046, 1, 64, 16, 2, [19], None, 64, 1, True, True),         # as many heads as a call may have
+    ("float16", 40, 1, 1, 64, 16, 30, [30 + b for b in range(40)], None, 16, 1, False, True),
+    ("bfloat16", 30, 2, 2, 128, 8, 70, [70] * 30, [b * 3 for b in range(30)], 128, 2, True, True),
 ]
 
 
@@ -656,6 +662,13 @@ def test_captured_step_replays_with_new_lengths(torch):
             assert torch.equal(x, y)
     other.close()
     ia.close()
+
+
+@pytest.mark.parametrize("weight", [False, True])
+def test_forward_of_as_many_rows_as_a_call_may_have(torch, ia, weight):
+    c = Case(torch, 131, 2, 1, 64, 16, [700, 64], room=0)
+    got, wt, want, w = run_forward(torch, ia, c, 64, 64, [64, 33], weight=weight)
+    check_forward(torch, c, got, wt, want, w, 4096, "int8")
 
 
 def test_room_is_reserved_for_fewer_rows_too(torch):

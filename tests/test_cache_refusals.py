@@ -163,6 +163,42 @@ def test_appends_that_are_refused(ia, want, kw):
     assert rc == want and text and "host-only" not in text, (rc, text)
 
 
+def test_outputs_over_themselves_are_refused(ia):
+    """Inputs may have axes of stride 0, what is written may not; an axis of one element may have any stride."""
+    for i, s in ((0, 0), (0, 1), (1, 1), (0, 2)):
+        a = rope()
+        a.dst_stride[i][s] = 112
+        assert code(ia, "intattn_rope", a, None)[0] == BAD
+        a = rope()
+        a.src_stride[i][s] = 0
+        assert "host-only" in code(ia, "intattn_rope", a, None)[1]
+    for s in range(3):
+        assert code(ia, "intattn_cache_append", cache(), append(q_out_stride=(s, 48)), None)[0] == BAD
+        assert "host-only" in code(ia, "intattn_cache_append", cache(), append(q_stride=(s, 0)), None)[1]
+        assert code(ia, "intattn_cache_forward", cache(), forward(out_stride=(s, 48)), None)[0] == BAD
+        assert "host-only" in code(ia, "intattn_cache_forward", cache(), forward(q_stride=(s, 0)), None)[1]
+    for s in range(2):
+        for name in ("k_stride", "v_stride"):
+            flat = cache(**{name: (s, 0)})
+            assert code(ia, "intattn_cache_append", flat, append(), None)[0] == BAD
+            assert code(ia, "intattn_cache_evict", flat, evict(), None)[0] == BAD
+            assert "host-only" in code(ia, "intattn_cache_forward", flat, forward(), None)[1]
+        assert code(ia, "intattn_cache_append", cache(), append(weight=P, weight_stride=(s, 0)), None)[0] == BAD
+        assert code(ia, "intattn_cache_append", cache(), append(order=P, order_stride=(s, 0)), None)[0] == BAD
+        assert code(ia, "intattn_cache_forward", cache(), forward(weight=P, weight_out=P + 4096, weight_out_stride=(s, 0)), None)[0] == BAD
+        assert "host-only" in code(ia, "intattn_cache_forward", cache(), forward(weight=P, weight_out=P + 4096, weight_stride=(s, 0)), None)[1]
+        assert code(ia, "intattn_cache_evict", cache(), evict(weight_out=P + 4096, weight_out_stride=(s, 0)), None)[0] == BAD
+        assert code(ia, "intattn_cache_evict", cache(), evict(order=P, order_out=P + 4096, order_out_stride=(s, 0)), None)[0] == BAD
+    assert "host-only" in code(ia, "intattn_rope", one_token(), None)[1]
+
+
+def one_token():
+    a = rope(B=1, L=1)
+    for i in range(2):
+        a.dst_stride[i][0] = a.dst_stride[i][2] = 0
+    return a
+
+
 def test_calls_of_more_tokens_than_a_grid_has_workgroups(ia):
     """2^24 workgroups of 256 threads are 2^32 threads."""
     for B, L, want in ((4096, 4096, NOT), (4095, 4096, None), (1, 131071, None), (65535, 256, None), (65535, 257, NOT)):
