@@ -4,9 +4,8 @@
 // three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  Steps whose scores do not
 // fit have room for their indices there, and K of these is read again for them: with 32 sequences of 4000 to 12400 keys, 8 KV heads of
 // four rows and d 128, 135 us, 4.2 TB/s of the bytes that have to move (the three launches of attend_split.hip 144).  A workgroup
-// takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens (with weights, which all rows add to, one
-// block of 16 rows after another: 32 rows of 2 keys, 4 sequences, 13.6 us; without 8.2); its waves take every NW-th step of 64 keys and
-// meet at the maxima and at the sums.
+// takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens (what several blocks of rows draw from the
+// keys is added up by a second launch); its waves take every NW-th step of 64 keys and meet at the maxima and at the sums.
 #include "attend_common.h"
 
 #include <algorithm>
@@ -34,8 +33,12 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
     const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
     const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
-    const int held_rows = min(p.rows, 16), blk0 = gridDim.y > 1 ? blockIdx.y : 0, blk1 = gridDim.y > 1 ? blk0 + 1 : p.blocks;
-    float *const weight_out = p.weight ? p.weight_out + b * p.wost[0] + kvh * p.wost[1] : nullptr;
+    const int held_rows = min(p.rows, 16), blk = blockIdx.y;
+    // weights: the only block of rows writes them, of several each what its rows draw to a plane of its own
+    const float *const weight = p.weight && p.blocks == 1 ? p.weight + b * p.wst[0] + kvh * p.wst[1] : nullptr;
+    float *const weight_out = !p.weight ? nullptr
+                              : p.blocks == 1 ? p.weight_out + b * p.wost[0] + kvh * p.wost[1]
+                                              : p.drawn + ((int64_t)blockIdx.x * p.blocks + blk) * p.c.capacity;
     const int held_to = min(steps, p.held_steps);
     auto place = [&](int s) { // the lane's
         const int i = (s * 4 + kb) * held_rows + n;
@@ -43,205 +46,213 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     };
     if (steps == 0) { // no keys: zeros
         const int none[4] = {0, 0, 0, 0};
-        const int end = blk1 * 16 < p.rows ? blk1 * 16 : p.rows;
-        for (int i = blk0 * 4 * D + threadIdx.x; i < end * D / 4; i += 64 * NW) store_out<4>(p, 0.0f, 0, 31, out_row(p, b, kvh, 4 * i / D), 4 * i % D, none);
+        const int end = min(blk * 16 + 16, p.rows);
+        for (int i = blk * 4 * D + threadIdx.x; i < end * D / 4; i += 64 * NW) store_out<4>(p, 0.0f, 0, 31, out_row(p, b, kvh, 4 * i / D), 4 * i % D, none);
         return;
     }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
 
-    for (int blk = blk0; blk < blk1; ++blk) {
-        const int row = blk * 16 + n;
-        // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
-        // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
-        // them a wait could no longer count them
-        const float *const weight = !p.weight ? nullptr : blk == 0 ? p.weight + b * p.wst[0] + kvh * p.wst[1] : weight_out;
-        v4i a[BUF][4][KB], qf[KB];
-        bool there[BUF][4];
-        uint32_t v[BUF][16][KB];
-        float old[BUF];
-        auto ask_v = [&](int s, const Place &from, uint32_t (&vv)[16][KB], float &w) {
-            keys.load_v(from, lane, vv);
-            w = 0.0f;
-            if (weight) w = weight[min(s * 64 + lane, len - 1)]; // uniform
-        };
-        const int last = steps - 1;
-        Place pv[2];
-        PlaceK pk[2];
-        if constexpr (PIPE) {
+    const int row = blk * 16 + n;
+    // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
+    // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
+    // them a wait could no longer count them
+    v4i a[BUF][4][KB], qf[KB];
+    bool there[BUF][4];
+    uint32_t v[BUF][16][KB];
+    float old[BUF];
+    auto ask_v = [&](int s, const Place &from, uint32_t (&vv)[16][KB], float &w) {
+        keys.load_v(from, lane, vv);
+        w = 0.0f;
+        if (weight) w = weight[min(s * 64 + lane, len - 1)]; // uniform
+    };
+    const int last = steps - 1;
+    Place pv[2];
+    PlaceK pk[2];
+    if constexpr (PIPE) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + i * NW, last), lane);
+        for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + i * NW, last), lane);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) keys.load_k(pk[i], lane, a[i], there[i]);
+        for (int i = 0; i < 2; ++i) keys.load_k(pk[i], lane, a[i], there[i]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + (2 + i) * NW, last), lane);
-        } else {
-            pk[0] = keys.find_k(wave, lane);
-            pv[0] = keys.find_v(wave, lane);
+        for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + (2 + i) * NW, last), lane);
+    } else {
+        pk[0] = keys.find_k(wave, lane);
+        pv[0] = keys.find_v(wave, lane);
+        keys.load_k(pk[0], lane, a[0], there[0]);
+        ask_v(wave, pv[0], v[0], old[0]);
+    }
+    load_q<D>(p, b, kvh, row, kb, qf);
+    if (threadIdx.x < 16) {
+        RowParams rp = {1.0, 0.0f, 1, 0, 0, 31};
+        if (row < p.rows) {
+            const int t = row % p.L;
+            if (row_params(p, b, kvh * p.group + row / p.L, t, kvh, rp) && t < fresh) rp.limit = len - fresh + t + 1;
+        }
+        rowp[n] = rp;
+        row_max[n] = HIDDEN;
+        row_sum[n] = 0;
+    }
+    for (int i = threadIdx.x; i < 16 * ACC_ROW; i += 64 * NW) acc_sum[i] = 0;
+    lds_barrier();
+    const bool mine = n < held_rows;
+    const int limit = mine ? rowp[n].limit : 0x7fffffff;
+
+    // Q.K^T and row maxima
+    int top = HIDDEN;
+    auto take_k = [&](int s, const v4i (&ka)[4][KB], const bool (&kt)[4]) {
+        v4i sc[4];
+        step_scores<D>(ka, kt, qf, limit - (s * 64 + 16 * kb), kb, sc);
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
+        if (mine && s < held_to) {
+            int4 *at = place(s);
+#pragma unroll
+            for (int ii = 0; ii < 4; ++ii) at[ii] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
+        }
+    };
+    if constexpr (PIPE) {
+        for (int s = wave; s < steps; s += 2 * NW) {
+            take_k(s, a[0], there[0]);
             keys.load_k(pk[0], lane, a[0], there[0]);
-            ask_v(wave, pv[0], v[0], old[0]);
+            pk[0] = keys.find_k(min(s + 4 * NW, last), lane);
+            if (s + NW < steps) take_k(s + NW, a[1], there[1]);
+            keys.load_k(pk[1], lane, a[1], there[1]);
+            pk[1] = keys.find_k(min(s + 5 * NW, last), lane);
         }
-        load_q<D>(p, b, kvh, row, kb, qf);
-        if (threadIdx.x < 16) {
-            RowParams rp = {1.0, 0.0f, 1, 0, 0, 31};
-            if (row < p.rows) {
-                const int t = row % p.L;
-                if (row_params(p, b, kvh * p.group + row / p.L, t, kvh, rp) && t < fresh) rp.limit = len - fresh + t + 1;
-            }
-            rowp[n] = rp;
-            row_max[n] = HIDDEN;
-            row_sum[n] = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + i * NW, last), lane);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ask_v(min(wave + i * NW, last), pv[i], v[i], old[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + (2 + i) * NW, last), lane);
+    } else {
+        for (int s = wave; s < steps;) {
+            take_k(s, a[0], there[0]);
+            s += NW;
+            if (s < steps) keys.load_k(keys.find_k(s, lane), lane, a[0], there[0]);
         }
-        for (int i = threadIdx.x; i < 16 * ACC_ROW; i += 64 * NW) acc_sum[i] = 0;
-        lds_barrier();
-        const bool mine = n < held_rows;
-        const int limit = mine ? rowp[n].limit : 0x7fffffff;
+    }
+    top = max(top, __shfl_xor(top, 16));
+    top = max(top, __shfl_xor(top, 32));
+    if (kb == 0 && mine) atomicMax(&row_max[n], top);
+    lds_barrier();
 
-        // Q.K^T and row maxima
-        int top = HIDDEN;
-        auto take_k = [&](int s, const v4i (&ka)[4][KB], const bool (&kt)[4]) {
+    // indices and row sums: sixteen scores of a row to a thread, whichever wave they came from, so that all lanes have work
+    // (by the lanes that hold the rows it took 20 us of 115 at four rows and 8192 keys)
+    for (int i = threadIdx.x; i < held_to * 4 * held_rows; i += 64 * NW) {
+        const int r = i % held_rows;
+        int4 *const at = held + 4 * i;
+        const int c_int = rowp[r].c_int;
+        const uint32_t row_top = (uint32_t)row_max[r];
+        const double factor = rowp[r].factor;
+        int sum = 0;
+        uint32_t word[4];
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) {
+            const int4 x = at[ii];
+            const uint32_t away[4] = {row_top - (uint32_t)x.x, row_top - (uint32_t)x.y, row_top - (uint32_t)x.z, row_top - (uint32_t)x.w};
+            word[ii] = four_indices(away, c_int, factor, entry, sum);
+        }
+        at[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+        atomicAdd(&row_sum[r], sum);
+    }
+    if (held_to < steps) {
+        const int c_int = rowp[n].c_int;
+        const uint32_t row_top = (uint32_t)row_max[n];
+        const double factor = rowp[n].factor;
+        int sum = 0;
+        PlaceK at = keys.find_k(held_to + wave, lane);
+        for (int s = held_to + wave; s < steps; s += NW) {
             v4i sc[4];
-            step_scores<D>(ka, kt, qf, limit - (s * 64 + 16 * kb), kb, sc);
-#pragma unroll
-            for (int ii = 0; ii < 4; ++ii) top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
-            if (mine && s < held_to) {
-                int4 *at = place(s);
-#pragma unroll
-                for (int ii = 0; ii < 4; ++ii) at[ii] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
-            }
-        };
-        if constexpr (PIPE) {
-            for (int s = wave; s < steps; s += 2 * NW) {
-                take_k(s, a[0], there[0]);
-                keys.load_k(pk[0], lane, a[0], there[0]);
-                pk[0] = keys.find_k(min(s + 4 * NW, last), lane);
-                if (s + NW < steps) take_k(s + NW, a[1], there[1]);
-                keys.load_k(pk[1], lane, a[1], there[1]);
-                pk[1] = keys.find_k(min(s + 5 * NW, last), lane);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + i * NW, last), lane);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) ask_v(min(wave + i * NW, last), pv[i], v[i], old[i]);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + (2 + i) * NW, last), lane);
-        } else {
-            for (int s = wave; s < steps;) {
-                take_k(s, a[0], there[0]);
-                s += NW;
-                if (s < steps) keys.load_k(keys.find_k(s, lane), lane, a[0], there[0]);
-            }
-        }
-        top = max(top, __shfl_xor(top, 16));
-        top = max(top, __shfl_xor(top, 32));
-        if (kb == 0 && mine) atomicMax(&row_max[n], top);
-        lds_barrier();
-
-        // indices and row sums: sixteen scores of a row to a thread, whichever wave they came from, so that all lanes have work
-        // (by the lanes that hold the rows it took 20 us of 115 at four rows and 8192 keys)
-        for (int i = threadIdx.x; i < held_to * 4 * held_rows; i += 64 * NW) {
-            const int r = i % held_rows;
-            int4 *const at = held + 4 * i;
-            const int c_int = rowp[r].c_int;
-            const uint32_t row_top = (uint32_t)row_max[r];
-            const double factor = rowp[r].factor;
-            int sum = 0;
+            keys.load_k(at, lane, a[0], there[0]);
+            at = keys.find_k(s + NW, lane);
+            step_scores<D>(a[0], there[0], qf, limit - (s * 64 + 16 * kb), kb, sc);
+            if (!mine) continue;
             uint32_t word[4];
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) {
-                const int4 x = at[ii];
-                const uint32_t away[4] = {row_top - (uint32_t)x.x, row_top - (uint32_t)x.y, row_top - (uint32_t)x.z, row_top - (uint32_t)x.w};
+                const uint32_t away[4] = {row_top - (uint32_t)sc[ii][0], row_top - (uint32_t)sc[ii][1], row_top - (uint32_t)sc[ii][2], row_top - (uint32_t)sc[ii][3]};
                 word[ii] = four_indices(away, c_int, factor, entry, sum);
             }
-            at[0] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
-            atomicAdd(&row_sum[r], sum);
+            *place(s) = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
         }
-        if (held_to < steps) {
-            const int c_int = rowp[n].c_int;
-            const uint32_t row_top = (uint32_t)row_max[n];
-            const double factor = rowp[n].factor;
-            int sum = 0;
-            PlaceK at = keys.find_k(held_to + wave, lane);
-            for (int s = held_to + wave; s < steps; s += NW) {
-                v4i sc[4];
-                keys.load_k(at, lane, a[0], there[0]);
-                at = keys.find_k(s + NW, lane);
-                step_scores<D>(a[0], there[0], qf, limit - (s * 64 + 16 * kb), kb, sc);
-                if (!mine) continue;
-                uint32_t word[4];
-#pragma unroll
-                for (int ii = 0; ii < 4; ++ii) {
-                    const uint32_t away[4] = {row_top - (uint32_t)sc[ii][0], row_top - (uint32_t)sc[ii][1], row_top - (uint32_t)sc[ii][2], row_top - (uint32_t)sc[ii][3]};
-                    word[ii] = four_indices(away, c_int, factor, entry, sum);
-                }
-                *place(s) = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
-            }
-            if (mine) atomicAdd(&row_sum[n], sum);
-        }
-        lds_barrier();
-        // tables of the rows
-        for (int i = threadIdx.x; i < held_rows * (p.top + 1); i += 64 * NW) {
-            const int r = i / (p.top + 1), idx = i & p.top; // (2^b entries)
-            const uint32_t e = row_max[r] != HIDDEN ? entry[idx] : 0u, S = (uint32_t)max(row_sum[r], 1);
-            prob[r][idx] = (uint8_t)prob_u8(e, S, __builtin_amdgcn_rcpf((float)(2u * S)));
-            if (weight_out) share[r][idx] = (float)e / (float)S;
-        }
-        lds_barrier();
-
-        // P.V and the keys' weights
-        v4i acc[CT];
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
-        auto take_v = [&](int s, const uint32_t (&vv)[16][KB], float before) {
-            uint32_t word[4] = {0, 0, 0, 0};
-            if (mine) {
-                const int4 x = *place(s);
-                word[0] = (uint32_t)x.x, word[1] = (uint32_t)x.y, word[2] = (uint32_t)x.z, word[3] = (uint32_t)x.w;
-            }
-            v4i pf = {0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const uint32_t pr = prob[n][(word[j / 4] >> (8 * (j & 3))) & 0xffu];
-                pf[j / 4] |= (int)(pr << (8 * (j & 3)));
-            }
-            if (!mine) pf = v4i{0, 0, 0, 0};
-            step_pv<D>(vv, pf, acc);
-            if (weight_out) { // uniform
-                if (mine) widx[wave][n * 4 + kb] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
-                const float drawn = drawn_by((const uint8_t *)widx[wave], share, held_rows, lane);
-                const int slot = s * 64 + lane;
-                if (slot < len) weight_out[slot] = (blk == 0 ? p.decay * before : before) + drawn; // (further rows add to what the lane itself wrote)
-            }
-        };
-        if constexpr (PIPE) {
-            for (int s = wave; s < steps; s += 2 * NW) {
-                take_v(s, v[0], old[0]);
-                ask_v(min(s + 2 * NW, last), pv[0], v[0], old[0]);
-                pv[0] = keys.find_v(min(s + 4 * NW, last), lane);
-                if (s + NW < steps) take_v(s + NW, v[1], old[1]);
-                ask_v(min(s + 3 * NW, last), pv[1], v[1], old[1]);
-                pv[1] = keys.find_v(min(s + 5 * NW, last), lane);
-            }
-        } else {
-            for (int s = wave; s < steps;) {
-                take_v(s, v[0], old[0]);
-                s += NW;
-                if (s < steps) ask_v(s, keys.find_v(s, lane), v[0], old[0]);
-            }
-        }
-        if (mine && wave < steps) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
-        }
-        lds_barrier();
-        for (int i = threadIdx.x; i < held_rows * D / 4; i += 64 * NW) {
-            const int r = 4 * i / D, ch = 4 * i % D, g = blk * 16 + r;
-            const int *const a = &acc_sum[r * ACC_ROW + ch], four[4] = {a[0], a[1], a[2], a[3]};
-            if (g < p.rows) store_out<4>(p, rowp[r].unit, rowp[r].mult, rowp[r].shift, out_row(p, b, kvh, g), ch, four);
-        }
-        lds_barrier(); // before the next rows' parameters
+        if (mine) atomicAdd(&row_sum[n], sum);
     }
+    lds_barrier();
+    // tables of the rows
+    for (int i = threadIdx.x; i < held_rows * (p.top + 1); i += 64 * NW) {
+        const int r = i / (p.top + 1), idx = i & p.top; // (2^b entries)
+        const uint32_t e = row_max[r] != HIDDEN ? entry[idx] : 0u, S = (uint32_t)max(row_sum[r], 1);
+        prob[r][idx] = (uint8_t)prob_u8(e, S, __builtin_amdgcn_rcpf((float)(2u * S)));
+        if (weight_out) share[r][idx] = (float)e / (float)S;
+    }
+    lds_barrier();
+
+    // P.V and the keys' weights
+    v4i acc[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
+    auto take_v = [&](int s, const uint32_t (&vv)[16][KB], float before) {
+        uint32_t word[4] = {0, 0, 0, 0};
+        if (mine) {
+            const int4 x = *place(s);
+            word[0] = (uint32_t)x.x, word[1] = (uint32_t)x.y, word[2] = (uint32_t)x.z, word[3] = (uint32_t)x.w;
+        }
+        v4i pf = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t pr = prob[n][(word[j / 4] >> (8 * (j & 3))) & 0xffu];
+            pf[j / 4] |= (int)(pr << (8 * (j & 3)));
+        }
+        if (!mine) pf = v4i{0, 0, 0, 0};
+        step_pv<D>(vv, pf, acc);
+        if (weight_out) { // uniform
+            if (mine) widx[wave][n * 4 + kb] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
+            const float drawn = drawn_by((const uint8_t *)widx[wave], share, held_rows, lane);
+            const int slot = s * 64 + lane;
+            if (slot < len) weight_out[slot] = p.decay * before + drawn;
+        }
+    };
+    if constexpr (PIPE) {
+        for (int s = wave; s < steps; s += 2 * NW) {
+            take_v(s, v[0], old[0]);
+            ask_v(min(s + 2 * NW, last), pv[0], v[0], old[0]);
+            pv[0] = keys.find_v(min(s + 4 * NW, last), lane);
+            if (s + NW < steps) take_v(s + NW, v[1], old[1]);
+            ask_v(min(s + 3 * NW, last), pv[1], v[1], old[1]);
+            pv[1] = keys.find_v(min(s + 5 * NW, last), lane);
+        }
+    } else {
+        for (int s = wave; s < steps;) {
+            take_v(s, v[0], old[0]);
+            s += NW;
+            if (s < steps) ask_v(s, keys.find_v(s, lane), v[0], old[0]);
+        }
+    }
+    if (mine && wave < steps) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicAdd(&acc_sum[n * ACC_ROW + CT * (4 * kb + i) + c], acc[c][i]);
+    }
+    lds_barrier();
+    for (int i = threadIdx.x; i < held_rows * D / 4; i += 64 * NW) {
+        const int r = 4 * i / D, ch = 4 * i % D, g = blk * 16 + r;
+        const int *const a = &acc_sum[r * ACC_ROW + ch], four[4] = {a[0], a[1], a[2], a[3]};
+        if (g < p.rows) store_out<4>(p, rowp[r].unit, rowp[r].mult, rowp[r].shift, out_row(p, b, kvh, g), ch, four);
+    }
+}
+
+// Weights where a KV head has several blocks of rows: what they have drawn, block by block.
+__global__ __launch_bounds__(256) void attend_weights_kernel(const AttendParams p)
+{
+    const int b = blockIdx.y / p.c.Hkv, kvh = blockIdx.y % p.c.Hkv, slot = blockIdx.x * 256 + threadIdx.x;
+    if (slot >= cache_len(p.c, b)) return;
+    const float *const of = p.drawn + (int64_t)blockIdx.y * p.blocks * p.c.capacity + slot;
+    float drawn = 0.0f;
+#pragma unroll 8
+    for (int blk = 0; blk < p.blocks; ++blk) drawn += of[(int64_t)blk * p.c.capacity];
+    p.weight_out[b * p.wost[0] + kvh * p.wost[1] + slot] = p.decay * p.weight[b * p.wst[0] + kvh * p.wst[1] + slot] + drawn;
 }
 
 } // namespace
@@ -260,31 +271,32 @@ static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_
 
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
 // launch takes 8, a third or half for each step of the longest sequence in its workgroup and a little for its rows, or what all bytes
-// take through the chip; with weights it takes blocks of rows one after another.  Three take 17 and what all bytes need, and further ones
-// for more than one block of rows.  (8 KV heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15,
-// 1 x 2048 19.3 and 18.3, 8 x 1024 15 and 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; one
-// KV head of 32 rows, d 64, 32 x 1 .. 4380 keys 30 and 28.)
+// take through the chip.  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV
+// heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15, 1 x 2048 19.3 and 18.3, 8 x 1024 15 and
+// 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; one KV head of 32 rows, d 64, 32 x 1 ..
+// 4380 keys 30 and 28.)
 static bool split_serves(const AttendParams &p, int d, bool weight)
 {
     if (held_steps(p) < 0) return true;
     const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv * p.blocks, size = d / 128.0;
-    const int turns = weight ? p.blocks : 1;
     const double step = (steps <= 32 ? 0.35 : 0.48) * size + 0.0065 * std::min(p.rows, 16);
-    const double one = 8.0 + 5.6 * (turns - 1) + std::max(steps * turns * step, 0.0031 * all * size);
+    const double one = 8.0 + (p.blocks > 1 && weight ? 4.0 : 0.0) + std::max(steps * step, 0.0031 * all * size);
     const double three = 17.0 + (p.blocks > 1 ? weight ? 15.0 : 6.0 : 0.0) + 0.0035 * all * size;
     return three < one;
 }
+
+// room: what each block of rows draws, [group][block][capacity]
+static int64_t drawn_room(const AttendParams &p, bool weight) { return weight && p.blocks > 1 ? 4 * (int64_t)p.c.B * p.c.Hkv * p.blocks * p.c.capacity : 0; }
 
 template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, void *stream)
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
-    const int parts = p.weight ? 1 : p.blocks; // (blocks of rows add to weights one after another)
     // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
     // Four where a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their way while the other
     // looks up indices (eight waves and four, us: 512 of 100 .. 3700 keys 87.1, 69.1; 320 of 1000 .. 3000 56.6, 48.0; 2048 of 300 ..
     // 1000 110, 82; but 272 of 300 .. 1800 32.0, 35.4).
-    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * parts;
+    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
     const bool two = groups >= 320 && held_bytes(p) <= 60 * 1024;
     const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
     // two steps in flight: 8 groups, 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1; 512 groups of four waves,
@@ -294,11 +306,15 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
     if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
     else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;
     else kernel = pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)parts), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
                        (hipStream_t)stream, p);
+    if (drawn_room(p, p.weight) > 0)
+        hipLaunchKernelGGL(attend_weights_kernel, dim3((uint32_t)((p.c.capacity + 255) / 256), (uint32_t)(p.c.B * p.c.Hkv)), dim3(256), 0, (hipStream_t)stream, p);
 }
 
-int64_t attend_room(const AttendParams &p, int d) { return split_serves(p, d, p.weight) ? attend_split_room(p, d, nullptr, nullptr) : 0; }
+static int64_t room_of(const AttendParams &p, int d, bool weight) { return split_serves(p, d, weight) ? attend_split_room(p, d, nullptr, nullptr) : drawn_room(p, weight); }
+
+int64_t attend_room(const AttendParams &p, int d) { return room_of(p, d, p.weight); }
 
 int64_t attend_room_upto(const AttendParams &p_, int d)
 {
@@ -306,14 +322,16 @@ int64_t attend_room_upto(const AttendParams &p_, int d)
     int64_t most = 0;
     for (p.blocks = 1; p.blocks <= p_.blocks; ++p.blocks) { // (the choice differs between numbers of blocks)
         p.rows = std::min(p_.rows, 16 * p.blocks);
-        if (split_serves(p, d, false) || split_serves(p, d, true)) most = std::max(most, attend_split_room(p, d, nullptr, nullptr));
+        most = std::max(most, std::max(room_of(p, d, false), room_of(p, d, true)));
     }
     return most;
 }
 
-int launch_attend(const AttendParams &p, int d, void *room, void *stream)
+int launch_attend(const AttendParams &p_, int d, void *room, void *stream)
 {
-    if (split_serves(p, d, p.weight)) return launch_attend_split(p, d, room, stream);
+    if (split_serves(p_, d, p_.weight)) return launch_attend_split(p_, d, room, stream);
+    AttendParams p = p_;
+    p.drawn = (float *)room;
     const bool whole = whole_pages(p.c, d);
     if (d == 64) whole ? launch_waves<64, true>(p, stream) : launch_waves<64, false>(p, stream);
     else whole ? launch_waves<128, true>(p, stream) : launch_waves<128, false>(p, stream);

@@ -87,7 +87,9 @@ struct AttendParams {
     int32_t top;
     double clip, sqrt_d;
     uint32_t lut[16];
-    int32_t held_steps;        // one launch: steps of 64 keys whose scores LDS holds
+    // one launch: steps of 64 keys whose scores LDS holds; room for what blocks of rows draw from the keys, if there are several
+    int32_t held_steps;
+    float *drawn;
     // keys split over workgroups (attend_split.hip): steps of a sequence of capacity slots, and for each launch the steps of a
     // workgroup and the workgroups of a sequence.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks of that
     // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], sums and parameters
