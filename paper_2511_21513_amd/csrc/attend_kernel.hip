@@ -270,8 +270,8 @@ static int held_steps(const AttendParams &p)
 static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_steps(p) + 3 * held_steps(p)); }
 
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
-// launch takes 8, a third or half for each step of the longest sequence in its workgroup and a little for its rows, or what all bytes
-// take through the chip.  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV
+// launch takes 8, a third or half for each step of the longest sequence in its workgroup (more where pages are not whole runs of 16
+// keys) and a little for its rows, or what all bytes take through the chip.  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV
 // heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15, 1 x 2048 19.3 and 18.3, 8 x 1024 15 and
 // 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; one KV head of 32 rows, d 64, 32 x 1 ..
 // 4380 keys 30 and 28.)
@@ -279,7 +279,7 @@ static bool split_serves(const AttendParams &p, int d, bool weight)
 {
     if (held_steps(p) < 0) return true;
     const double steps = most_steps(p), all = steps * p.c.B * p.c.Hkv * p.blocks, size = d / 128.0;
-    const double step = (steps <= 32 ? 0.35 : 0.48) * size + 0.0065 * std::min(p.rows, 16);
+    const double step = ((steps <= 32 ? 0.35 : 0.48) * size + 0.0065 * std::min(p.rows, 16)) * (whole_pages(p.c, d) ? 1.0 : 1.3);
     const double one = 8.0 + (p.blocks > 1 && weight ? 4.0 : 0.0) + std::max(steps * step, 0.0031 * all * size);
     const double three = 17.0 + (p.blocks > 1 ? weight ? 15.0 : 6.0 : 0.0) + 0.0035 * all * size;
     return three < one;
