@@ -280,16 +280,14 @@ def _rows(t, what, dtype, shape, device):
     return st
 
 
-def _like(t, dtype):
+def _like(torch, t, dtype):
     """A new tensor in the memory order of a [B, H, L, d] tensor, where its rows can be written in pieces of 16 bytes, and its strides."""
-    import torch
-
     out = torch.empty_like(t, dtype=dtype)
-    st = out.stride()
-    if st[3] == 1 and not (st[0] | st[1] | st[2]) & 15:
-        return out, st
+    s0, s1, s2, s3 = out.stride()
+    if s3 == 1 and not (s0 | s1 | s2) & 15:
+        return out, s0, s1, s2
     out = torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)  # (a broadcast axis of t may end up innermost)
-    return out, out.stride()
+    return out, *out.stride()[:3]
 
 
 def _slots(t, what, dtype, B, Hkv, slots, device):
@@ -302,10 +300,8 @@ def _slots(t, what, dtype, B, Hkv, slots, device):
     return t.stride()[:2]
 
 
-def _rotation(B, L, device, pos, freq, axis, pairing, inverse):
+def _rotation(torch, B, L, device, pos, freq, axis, pairing, inverse):
     """The fields of intattn_rotary."""
-    import torch
-
     if pos.dim() == 2:
         pos = pos[None]
     _check(pos, "pos", torch.int32, (pos.shape[0], B, L), device)
@@ -624,28 +620,39 @@ class IntAttn:
 
         one = torch.is_tensor(x)
         xs = (x,) if one else x
-        outs = None if out is None else [out] if torch.is_tensor(out) else list(out)
-        if not 1 <= len(xs) <= 2 or (outs is not None and len(outs) != len(xs)):
+        n = len(xs)
+        if not 1 <= n <= 2:
             raise ValueError("one tensor or two, and as many outputs")
         a, b = xs[0], xs[-1]
-        B, H, L, d = a.shape
-        dtype, dev, es, H2 = a.dtype, a.get_device(), a.element_size(), b.shape[1]
+        B, H, L, d = shape = a.shape
+        dtype, dev, es = a.dtype, a.get_device(), a.element_size()
         code = _float_types().get(dtype)
         if code is None:
             raise ValueError("expected float32/float16/bfloat16 tensors")
-        s0, s1, s2, _ = _rows(a, "x", dtype, a.shape, dev)
-        t0, t1, t2, _ = _rows(b, "x", dtype, (B, H2, L, d), dev)
-        if outs is None:
-            new = [_like(t, dtype) for t in xs]
-            outs, (o0, o1, o2, _), (p0, p1, p2, _) = [n[0] for n in new], new[0][1], new[-1][1]
+        s0, s1, s2, _ = _rows(a, "x", dtype, shape, dev)
+        if n == 2:
+            H2 = b.shape[1]
+            t0, t1, t2, _ = _rows(b, "x", dtype, (B, H2, L, d), dev)
         else:
-            o0, o1, o2, _ = _rows(outs[0], "out", dtype, a.shape, dev)
-            p0, p1, p2, _ = _rows(outs[-1], "out", dtype, b.shape, dev)
-        args = _ROPE.pack(B, L, d, code, H, 0 if len(xs) == 1 else H2, a.data_ptr(), b.data_ptr(), outs[0].data_ptr(), outs[-1].data_ptr(),
+            H2, t0, t1, t2 = 0, s0, s1, s2
+        if out is None:
+            o, o0, o1, o2 = p, p0, p1, p2 = _like(torch, a, dtype)
+            if n == 2:
+                p, p0, p1, p2 = _like(torch, b, dtype)
+            out = o if one else [o, p][:n]
+        else:
+            outs = [out] if torch.is_tensor(out) else list(out)
+            if len(outs) != n:
+                raise ValueError("one tensor or two, and as many outputs")
+            o, p = outs[0], outs[-1]
+            o0, o1, o2, _ = _rows(o, "out", dtype, shape, dev)
+            p0, p1, p2, _ = _rows(p, "out", dtype, b.shape, dev)
+            out = o if one else outs
+        args = _ROPE.pack(B, L, d, code, H, H2, a.data_ptr(), b.data_ptr(), o.data_ptr(), p.data_ptr(),
                           s0 * es, s1 * es, s2 * es, t0 * es, t1 * es, t2 * es, o0 * es, o1 * es, o2 * es, p0 * es, p1 * es, p2 * es,
-                          *_rotation(B, L, dev, pos, freq, axis, pairing, inverse))
+                          *_rotation(torch, B, L, dev, pos, freq, axis, pairing, inverse))
         self._done(self._lib.intattn_rope(self._ctx, args, self._stream(dev, stream)))
-        return outs[0] if one else outs
+        return out
 
     def cache_append(self, cache: PagedCache, k, v, q=None, *, n_new=None, pos=None, freq=None, axis=None, pairing="adjacent",
                      weight=None, order=None, first=None, q_out=None, q_scale=None, stream=None):
@@ -667,7 +674,7 @@ class IntAttn:
             Hq = q.shape[1]
             q0, q1, q2, _ = _rows(q, "q", dtype, (B, Hq, L, d), dev)
             if q_out is None:
-                q_out, (o0, o1, o2, _) = _like(q, torch.int8)
+                q_out, o0, o1, o2 = _like(torch, q, torch.int8)
             else:
                 o0, o1, o2, _ = _rows(q_out, "q_out", torch.int8, (B, Hq, L, d), dev)
             if q_scale is None:
@@ -681,7 +688,7 @@ class IntAttn:
                       *_slots(order, "order", torch.int32, B, cache.Hkv, cache.capacity, dev))
         args = _APPEND.pack(L, Hq, code, 0, _ptr(q), k.data_ptr(), v.data_ptr(), q0 * es, q1 * es, q2 * es, k0 * es, k1 * es, k2 * es,
                             v0 * es, v1 * es, v2 * es, _ptr(n_new), _ptr(q_out) if Hq else 0, o0, o1, o2, _ptr(q_scale) if Hq else 0,
-                            *(_NO_ROTATION if pos is None else _rotation(B, L, dev, pos, freq, axis, pairing, False)), *planes)
+                            *(_NO_ROTATION if pos is None else _rotation(torch, B, L, dev, pos, freq, axis, pairing, False)), *planes)
         self._done(self._lib.intattn_cache_append(self._ctx, cache._ref, args, self._stream(dev, stream)))
         return (q_out, q_scale) if q is not None else None
 
@@ -704,7 +711,7 @@ class IntAttn:
         if code is None:
             raise ValueError("out must be float32/float16/bfloat16/int8")
         if out is None:
-            out, (o0, o1, o2, _) = _like(q, dtype)
+            out, o0, o1, o2 = _like(torch, q, dtype)
         else:
             o0, o1, o2, _ = _rows(out, "out", dtype, shape, dev)
         es = out.element_size()
