@@ -14,12 +14,23 @@ namespace {
 constexpr int PROB = 68; // bytes of a row's probabilities in LDS: rows start in banks of their own
 constexpr int HIDDEN = (int)0x80000000; // further below any row maximum than any clip threshold
 
-// c_int, index factor and output of one row, with the host's arithmetic; false where a scale is unusable
-__device__ __forceinline__ bool row_params(const AttendParams &p, int b, int head, int t, int kvh, RowParams &rp)
+struct RowScales {
+    float q, k, v, out;
+};
+__device__ __forceinline__ RowScales row_scales(const AttendParams &p, int b, int head, int t, int kvh)
 {
-    const float sq = p.scale_q[((int64_t)b * p.Hq + head) * p.L + t];
-    const float sk = p.c.scale_k[p.c.per_head ? kvh : 0], sv = p.c.scale_v[p.c.per_head ? kvh : 0];
-    const float so = p.out_type == 3 && p.scale_out ? p.scale_out[p.out_per_head ? head : 0] : sv;
+    RowScales s;
+    s.q = p.scale_q[((int64_t)b * p.Hq + head) * p.L + t];
+    s.k = p.c.scale_k[p.c.per_head ? kvh : 0];
+    s.v = p.c.scale_v[p.c.per_head ? kvh : 0];
+    s.out = p.out_type == 3 && p.scale_out ? p.scale_out[p.out_per_head ? head : 0] : s.v;
+    return s;
+}
+
+// c_int, index factor and output of one row, with the host's arithmetic; false where a scale is unusable
+__device__ __forceinline__ bool row_params(const AttendParams &p, const RowScales &s, RowParams &rp)
+{
+    const float sq = s.q, sk = s.k, sv = s.v, so = s.out;
     bool ok = good_cache_scale(sq) && good_cache_scale(sk) && good_cache_scale(sv) && good_cache_scale(so);
     double c = 1.0;
     if (ok) {

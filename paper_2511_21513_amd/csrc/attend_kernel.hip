@@ -29,11 +29,21 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     extern __shared__ int4 held[];
     __shared__ int4 widx[NW][64];               // indices of a wave's step
 
-    const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv;
+    const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv, blk = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
-    const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
     const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
-    const int held_rows = min(p.rows, 16), blk = blockIdx.y;
+    // (asked for before the length is known, and the scales before keys that a wait for them would have to wait for as well)
+    const int row = blk * 16 + n, head = kvh * p.group + row / p.L, t = row % p.L;
+    RowScales scales;
+    if (threadIdx.x < 16 && row < p.rows) scales = row_scales(p, b, head, t, kvh);
+    Place pv[2];
+    PlaceK pk[2];
+    if constexpr (!PIPE) {
+        pk[0] = keys.find_k(wave, lane);
+        pv[0] = keys.find_v(wave, lane);
+    }
+    const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
+    const int held_rows = min(p.rows, 16);
     // weights: the only block of rows writes them, of several each what its rows draw to a plane of its own
     const float *const weight = p.weight && p.blocks == 1 ? p.weight + b * p.wst[0] + kvh * p.wst[1] : nullptr;
     float *const weight_out = !p.weight ? nullptr
@@ -52,7 +62,6 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
 
-    const int row = blk * 16 + n;
     // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
     // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
     // them a wait could no longer count them
@@ -66,8 +75,6 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
         if (weight) w = weight[min(s * 64 + lane, len - 1)]; // uniform
     };
     const int last = steps - 1;
-    Place pv[2];
-    PlaceK pk[2];
     if constexpr (PIPE) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + i * NW, last), lane);
@@ -76,18 +83,13 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
 #pragma unroll
         for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + (2 + i) * NW, last), lane);
     } else {
-        pk[0] = keys.find_k(wave, lane);
-        pv[0] = keys.find_v(wave, lane);
         keys.load_k(pk[0], lane, a[0], there[0]);
         ask_v(wave, pv[0], v[0], old[0]);
     }
     load_q<D>(p, b, kvh, row, kb, qf);
     if (threadIdx.x < 16) {
         RowParams rp = {1.0, 0.0f, 1, 0, 0, 31};
-        if (row < p.rows) {
-            const int t = row % p.L;
-            if (row_params(p, b, kvh * p.group + row / p.L, t, kvh, rp) && t < fresh) rp.limit = len - fresh + t + 1;
-        }
+        if (row < p.rows && row_params(p, scales, rp) && t < fresh) rp.limit = len - fresh + t + 1;
         rowp[n] = rp;
         row_max[n] = HIDDEN;
         row_sum[n] = 0;

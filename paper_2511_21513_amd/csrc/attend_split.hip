@@ -54,7 +54,7 @@ template <int D, bool WHOLE, bool ONE> __global__ __launch_bounds__(SNT) void ca
         for (int i = threadIdx.x; i < SROWS && blk0 * 16 + i < p.rows; i += SNT) { // for the other launches
             const int row = blk0 * 16 + i;
             RowParams rp;
-            rp.limit = row_params(p, gr.b, gr.kvh * p.group + row / p.L, row % p.L, gr.kvh, rp);
+            rp.limit = row_params(p, row_scales(p, gr.b, gr.kvh * p.group + row / p.L, row % p.L, gr.kvh), rp);
             p.row_params[(int64_t)g * p.rows + row] = rp;
         }
     }
