@@ -7,15 +7,16 @@
 // the (len - keep)-th smallest in it.  It starts at the least and the greatest weight of the keys that are not held; a pass counts the
 // keys in 2048 equal parts of the interval, so that weights of all sizes spread over the parts, and once 256 keys are left, mostly
 // after one pass, they are compared with each other.  Of equal keys the lowest slots leave.  No sort, and nothing depends on the order in
-// which atomics arrive, because they count.  Each wave owns a run of slots; up to 16384 keys wait in LDS between the passes, more are
-// formed again.  Bound by the instructions and waits of one workgroup's passes over its keys.
+// which atomics arrive, because they count.  Each wave owns a run of slots; up to 24576 keys wait in registers between the passes, more
+// are formed again (16 sequences of 7000 to 10001 keys, 8 KV heads, 17.5 us, with the keys in LDS 19.2; 4 of 20000 25, formed again 46).
+// Bound by the instructions and waits of one workgroup's passes over its keys.
 #include "cache_common.h"
 
 namespace intattn {
 
 namespace {
 
-constexpr int EHOLD = 16384; // slots whose keys LDS holds
+constexpr int EHOLD = 24576; // slots whose keys registers hold
 constexpr int BINS = 2048, FEW = 256;
 
 constexpr uint64_t HELD = 1ull << 63;
@@ -46,7 +47,7 @@ template <int EWAVES> __device__ __forceinline__ int sum_of_waves(int mine, int 
     return all;
 }
 
-// ENT threads; HOLD: keys in LDS
+// ENT threads; HOLD: keys in registers
 template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_select_kernel(const EvictParams p)
 {
     constexpr int EWAVES = ENT / 64, PER = BINS / ENT;
@@ -55,7 +56,6 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
     __shared__ int free_keys[EWAVES];                              // and how many they are
     __shared__ uint64_t few[FEW], chosen_key;
     __shared__ unsigned long long first_key, last_key;
-    extern __shared__ uint64_t key_of[]; // HOLD: of slot s0 + 64 i at i ENT + thread
     const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int len = cache_len(p.c, b);
     const int rounds = (len + ENT - 1) / ENT, s0 = wave * rounds * 64 + lane; // slots s0 + 64 i of this thread
@@ -75,11 +75,15 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
         lightest = min(lightest, out ? 0xffffffffu : (uint32_t)(k >> 31));
         heaviest = max(heaviest, out ? 0u : (uint32_t)(k >> 31));
     };
-    // Keys to LDS (behind the last: above any), and planes of their own take what lies below keep as it is; gaps are filled by the
+    // The keys (behind the last: above any), and planes of their own take what lies below keep as it is; gaps are filled by the
     // next launch.
-    constexpr int AT_ONCE = 8; // loads of a thread in flight
+    constexpr int MOST = ENT == 1024 ? EHOLD / 1024 : 8, AT_ONCE = 8; // rounds where keys are held; loads of a thread in flight
+    constexpr int BATCHES = HOLD ? MOST / AT_ONCE : 1; // that are told apart, because registers have no index
+    uint64_t key[HOLD ? MOST : 1];
     const int under = min(len, p.keep);
-    for (int i0 = 0; i0 < rounds; i0 += AT_ONCE) {
+#pragma unroll BATCHES
+    for (int i0 = 0; i0 < (HOLD ? MOST : rounds); i0 += AT_ONCE) {
+        if (i0 >= rounds) break;
         float w[AT_ONCE];
         int o[AT_ONCE];
 #pragma unroll
@@ -95,7 +99,7 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
             if (i0 + u >= rounds) break;
             const uint64_t k = s < len ? sort_key(w[u], o[u], p.sink, newest) : ~0ull;
             range(k);
-            if constexpr (HOLD) key_of[(i0 + u) * ENT + tid] = k;
+            if constexpr (HOLD) key[i0 + u] = k;
             if (copy_w && s < under) weight_out[s] = w[u];
             if (copy_o && s < under) order_out[s] = o[u];
         }
@@ -128,18 +132,24 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
 
     // f(slot, key, round) for each slot of the thread
     auto each = [&](auto f) {
-        constexpr int AT_ONCE = 4; // keys on their way
-        for (int i0 = 0; i0 < rounds; i0 += AT_ONCE) {
-            uint64_t k[AT_ONCE];
+        if constexpr (HOLD) {
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                const int i = min(i0 + u, rounds - 1), s = s0 + 64 * i, from = min(s, len - 1);
-                if constexpr (HOLD) k[u] = key_of[i * ENT + tid];
-                else k[u] = s < len ? sort_key(weight[from], order ? order[from] : from, p.sink, newest) : ~0ull;
+            for (int i = 0; i < MOST; ++i) {
+                if (i >= rounds) break;
+                f(s0 + 64 * i, key[i], i);
             }
+        } else {
+            for (int i0 = 0; i0 < rounds; i0 += AT_ONCE) {
+                uint64_t k[AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u)
-                if (i0 + u < rounds) f(s0 + 64 * (i0 + u), k[u], i0 + u);
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int s = s0 + 64 * min(i0 + u, rounds - 1), from = min(s, len - 1);
+                    k[u] = s < len ? sort_key(weight[from], order ? order[from] : from, p.sink, newest) : ~0ull;
+                }
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u)
+                    if (i0 + u < rounds) f(s0 + 64 * (i0 + u), k[u], i0 + u);
+            }
         }
     };
 
@@ -269,7 +279,7 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
         return gone;
     };
     int gaps = 0, movers = 0, seen = equals;
-    uint32_t is_gap = 0, is_mover = 0; // of the thread, a bit for each round (HOLD: at most 16 of them)
+    uint32_t is_gap = 0, is_mover = 0; // of the thread, a bit for each round (HOLD: at most 24 of them)
     each([&](int s, uint64_t k, int i) {
         const bool gone = leaves(k, seen), gap = gone && s < p.keep, mover = !gone && s < len && s >= p.keep;
         is_gap |= (uint32_t)gap << (i & 31);
@@ -358,9 +368,8 @@ int launch_evict(const EvictParams &p_, void *room, void *stream)
     // a workgroup of 512 threads up to 4096 slots: its barriers are cheaper
     const bool few = p.c.capacity <= 4096, hold = p.c.capacity <= EHOLD;
     const int threads = few ? 512 : 1024;
-    const size_t lds = hold ? (size_t)(p.c.capacity + threads - 1) / threads * threads * 8 : 0;
     void (*select)(const EvictParams) = few ? evict_select_kernel<512, true> : hold ? evict_select_kernel<1024, true> : evict_select_kernel<1024, false>;
-    hipLaunchKernelGGL(select, dim3((uint32_t)groups), dim3((uint32_t)threads), (uint32_t)lds, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(select, dim3((uint32_t)groups), dim3((uint32_t)threads), 0, (hipStream_t)stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
     const int fit = (p.max_moves + MOVES - 1) / MOVES;
