@@ -273,10 +273,10 @@ static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_
 
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
 // launch takes 8, a third or half for each step of the longest sequence in its workgroup (more where pages are not whole runs of 16
-// keys) and a little for its rows, or what all bytes take through the chip.  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV
-// heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15, 1 x 2048 19.3 and 18.3, 8 x 1024 15 and
-// 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 105 and 141; one KV head of 32 rows, d 64, 32 x 1 ..
-// 4380 keys 30 and 28.)
+// keys) and a little for its rows, or what all bytes take through the chip.  Three take 17 and what all bytes need.  Both have further
+// launches for more than one block of rows.  (8 KV heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and
+// 15, 1 x 2048 19.3 and 18.3, 8 x 1024 14 and 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 103 and 141;
+// one KV head of 32 rows, d 64, 32 x 1 .. 4380 keys 30 and 28.)
 static bool split_serves(const AttendParams &p, int d, bool weight)
 {
     if (held_steps(p) < 0) return true;
@@ -294,16 +294,16 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
-    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
-    // Four where a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their way while the other
-    // looks up indices (eight waves and four, us: 512 of 100 .. 3700 keys 87.1, 69.1; 320 of 1000 .. 3000 56.6, 48.0; 2048 of 300 ..
-    // 1000 110, 82; but 272 of 300 .. 1800 32.0, 35.4).
-    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
-    const bool two = groups >= 320 && held_bytes(p) <= 60 * 1024;
-    const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
     // two steps in flight: 8 groups, 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1; 512 groups of four waves,
     // 32 steps 52.6, 54.0; 57 steps 95.9, 90.3
     const bool pipe = most_steps(p) > 32;
+    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
+    // Four where a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their way while the other
+    // looks up indices (eight waves and four, us: 512 of 100 .. 3700 keys 86.1, 67.7; 320 of 1000 .. 3000 54.4, 47.8; 272 of 300 .. 3800
+    // 55.5, 57.6; with one step in flight, where registers are left for two of eight, 512 of 300 .. 1800 with eight rows 33.0, 39.4).
+    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
+    const bool two = pipe && groups >= 320 && held_bytes(p) <= 60 * 1024;
+    const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
     void (*kernel)(const AttendParams);
     if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
     else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;
