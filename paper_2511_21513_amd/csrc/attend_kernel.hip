@@ -294,14 +294,14 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
-    // two steps in flight: 8 groups, 16 steps 12.7 us without, 17.2 with; 64 steps 42.6, 40.4; 128 steps 88.3, 78.1; 512 groups of four waves,
-    // 32 steps 52.6, 54.0; 57 steps 95.9, 90.3
-    const bool pipe = most_steps(p) > 32;
-    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
-    // Four where a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their way while the other
-    // looks up indices (eight waves and four, us: 512 of 100 .. 3700 keys 86.1, 67.7; 320 of 1000 .. 3000 54.4, 47.8; 272 of 300 .. 3800
-    // 55.5, 57.6; with one step in flight, where registers are left for two of eight, 512 of 300 .. 1800 with eight rows 33.0, 39.4).
+    // two steps in flight in the only workgroup of a compute unit (8 groups, 16 steps 12.7 us without, 17.2 with; 256 of up to 61, d 64,
+    // 28.9, 24.9; 128 of 128 88.3, 78.1); where there are more, later, because then registers are left for two workgroups of eight waves
+    // (320 of up to 47 steps 44.1, 47.6; 512 of up to 62, d 64, 73.8, 78.1; 272 of up to 60 50.8, 55.0)
     const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
+    const bool pipe = most_steps(p) > (groups > 256 ? 64 : 32);
+    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
+    // Four where two steps are in flight, a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their
+    // way while the other looks up indices (1024 of 300 .. 6000 keys, one row, d 64, eight waves 125 us, four 116).
     const bool two = pipe && groups >= 320 && held_bytes(p) <= 60 * 1024;
     const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
     void (*kernel)(const AttendParams);
