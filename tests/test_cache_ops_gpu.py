@@ -282,11 +282,11 @@ def test_forward_of_long_sequences(torch, ia, rows, d, page, n):
 
 
 @pytest.mark.parametrize("rows, d, page, lens", [(16, 64, 16, [2900, 0, 2112, 2113, 64]), (13, 128, 24, [2600, 2560, 1]), (9, 64, 64, [4800, 3840, 3000]), (4, 64, 16, [2300, 2048, 70, 0]),
-                                                  (4, 128, 16, [1500, 900]), (4, 64, 8, [2200, 65])])
+                                                  (4, 128, 16, [1500, 900]), (4, 64, 8, [2200, 65]), (2, 64, 64, [4200, 4096, 65])])
 def test_forward_of_long_sequences_among_many_short_ones(torch, ia, rows, d, page, lens):
     """Enough sequences for a workgroup each (176), or more than one to a compute unit (340), and a few of them with more scores than it
     holds."""
-    n = 340 if rows == 4 else 176
+    n = 340 if rows <= 4 else 176
     c = Case(torch, rows, n, 1, d, page, lens + [3] * (n - len(lens)), room=0)
     got, wt, want, w = run_forward(torch, ia, c, rows, 1, None)
     check_forward(torch, c, got, wt, want, w, rows, "int8")
