@@ -273,7 +273,8 @@ def _check(t, what, dtype, shape, device, contiguous=False):
 
 def _rows(t, what, dtype, shape, device):
     """The same for [B, H, L, d] tensors whose last axis has to be contiguous: their strides."""
-    _check(t, what, dtype, shape, device)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _check(t, what, dtype, shape, device)
     st = t.stride()
     if st[3] != 1:
         raise ValueError(f"{what}: the head dimension must be contiguous")
@@ -294,19 +295,23 @@ def _slots(t, what, dtype, B, Hkv, slots, device):
     """[B, Hkv, slots] planes (or None): the last axis is contiguous and holds every slot the call may touch."""
     if t is None:
         return 0, 0
-    if t.dim() != 3 or t.shape[2] < slots or t.stride(2) != 1:
+    n, st = t.shape, t.stride()
+    if len(n) != 3 or n[2] < slots or st[2] != 1:
         raise ValueError(f"{what} must be [B, Hkv, slots] with at least {slots} slots, contiguous")
-    _check(t, what, dtype, (B, Hkv, t.shape[2]), device)
-    return t.stride()[:2]
+    if t.dtype is not dtype or n[0] != B or n[1] != Hkv or t.get_device() != device:
+        _check(t, what, dtype, (B, Hkv, n[2]), device)
+    return st[0], st[1]
 
 
 def _rotation(torch, B, L, device, pos, freq, axis, pairing, inverse):
     """The fields of intattn_rotary."""
     if pos.dim() == 2:
         pos = pos[None]
-    _check(pos, "pos", torch.int32, (pos.shape[0], B, L), device)
-    n = freq.shape[0]
-    _check(freq, "freq", torch.float64, (n,), device, True)
+    axes, n = pos.shape[0], freq.shape[0]
+    if pos.dtype is not torch.int32 or pos.shape != (axes, B, L) or pos.get_device() != device:
+        _check(pos, "pos", torch.int32, (axes, B, L), device)
+    if freq.dtype is not torch.float64 or freq.dim() != 1 or freq.get_device() != device or not freq.is_contiguous():
+        _check(freq, "freq", torch.float64, (n,), device, True)
     if n > 128:
         raise ValueError("at most 128 rotated pairs")
     if pairing not in ("adjacent", "halves"):
@@ -315,7 +320,7 @@ def _rotation(torch, B, L, device, pos, freq, axis, pairing, inverse):
         axis = bytes(axis)  # (raises unless each is 0 .. 255; the library compares them with the axes)
         if len(axis) != n:
             raise ValueError("axis must name an axis for each pair")
-    return (2 * n, int(pairing == "halves"), pos.shape[0], int(bool(inverse)), pos.data_ptr(), *pos.stride(), freq.data_ptr(), axis or b"")
+    return (2 * n, int(pairing == "halves"), axes, int(bool(inverse)), pos.data_ptr(), *pos.stride(), freq.data_ptr(), axis or b"")
 
 
 class PagedCache:
