@@ -671,6 +671,38 @@ def test_forward_of_as_many_rows_as_a_call_may_have(torch, ia, weight):
     check_forward(torch, c, got, wt, want, w, 4096, "int8")
 
 
+def test_graphs_keep_their_room_when_it_is_outgrown(torch):
+    """Two graphs on one context, and an eager call in between that needs more room than the first was captured with."""
+    from paper_2511_21513_amd import binding
+
+    own = binding.IntAttn(device=0)
+    cases = []
+    for i, (n, rows) in enumerate(((2600, 4), (9000, 20))):
+        c = Case(torch, 141 + i, 1, 2, 64, 16, [n], room=0)
+        q, s, qt, st = c.queries(torch, 2 * rows, 1)
+        w0 = torch.rand((1, 2, c.width * 16), device="cuda")
+        w, out = torch.empty_like(w0), torch.empty((1, 2 * rows, 1, 64), dtype=torch.int8, device="cuda")
+        own.cache_forward(c.cache, qt, st, out=out, weight=w0, weight_out=w)  # grows the room
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            own.cache_forward(c.cache, qt, st, out=out, weight=w0, weight_out=w)
+        acc, want, real, new = plain.attend(q, s, c.k, c.v, c.table, c.lens, c.sk, c.sv, weight=w0.cpu().numpy())
+        cases.append((c, graph, out, w, want, new, rows, qt, st, w0))  # (what a graph reads has to live)
+    for turn in range(3):
+        for c, graph, out, w, want, new, rows, qt, st, w0 in cases:
+            out.fill_(5)
+            w.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert int((out.cpu().numpy() != want).sum()) == 0
+            assert (np.abs(wide(w) - new)[..., :c.lens[0]] <= (rows + 3) * 2.0 ** -24 * new[..., :c.lens[0]]).all()
+        out = own.cache_forward(cases[turn % 2][0].cache, cases[turn % 2][7], cases[turn % 2][8], dtype=torch.int8)
+        assert int((out.cpu().numpy() != cases[turn % 2][4]).sum()) == 0
+    del cases, graph
+    own.close()
+
+
 def test_room_is_reserved_for_fewer_rows_too(torch):
     """The kernels that a call takes depend on its rows and on whether weights are kept; a reservation holds for all of them."""
     from paper_2511_21513_amd import binding
