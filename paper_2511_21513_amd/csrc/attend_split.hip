@@ -394,7 +394,7 @@ static void plan(AttendParams &p)
     auto whole = [](int32_t steps) { return (steps + SWAVES - 1) / SWAVES * SWAVES; };
     p.score_steps = whole(steps_of(16384, 4, 256));
     p.lookup_steps = steps_of(1536, p.rows <= 16 ? 8 : std::max(1, 128 / p.rows), 256);
-    p.chunk_steps = whole(steps_of(3072, 8, 32));
+    p.chunk_steps = whole(steps_of(3000, 8, 32));
     p.score_chunks = (p.steps + p.score_steps - 1) / p.score_steps;
     p.lookup_chunks = (p.steps + p.lookup_steps - 1) / p.lookup_steps;
     p.chunks = (p.steps + p.chunk_steps - 1) / p.chunk_steps;
