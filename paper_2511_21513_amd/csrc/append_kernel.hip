@@ -178,7 +178,7 @@ int launch_append(const AppendParams &p_, int d, int dtype, void *stream)
     p.by_pairs = fast_div((uint32_t)(p.r.rot > 0 ? p.r.rot / 2 : 1));
     // tokens of a workgroup where there are enough (8192 tokens, one, two, four and eight, us: d 128, 48 heads 40.6, 36.8, 38.2, 39.8; d 64,
     // 48 heads 28.7, 25.5, 24.1, 23.0; d 128, 8 heads 18.1, 14.8, 13.1, 12.8; 131 000 tokens, d 64, 3 heads 189, 100, 57.9, 41.9); the heads
-    // of a token over several workgroups where there are few
+    // of a token over several workgroups where there are few (32 tokens of 48 heads 5.4 us, in one workgroup each 6.1)
     const int units = d / (dtype == 0 ? 8 : 16), rows = ANT / units;
     p.tokens = tokens_of(all, p.heads * units, 4, p.r.rot, TOKENS);
     const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.heads + rows - 1) / rows;

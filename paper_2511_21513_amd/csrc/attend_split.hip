@@ -381,7 +381,8 @@ __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p
 
 // Steps of a workgroup in each launch, by the number of steps there can be (one row, 32 sequences of 4000 to 12400 keys, and one of
 // 30011, d 128, us): scores, short workgroups, 4: 59.0, 9.1; 16: 69.5, 11.0.  Lookup, 8: 12.9, 4.6; 32: 10.2, 5.3.  Values, where
-// each workgroup leaves accumulators to be joined, 4: 128, 31.8; 8: 87, 21.2; 16: 73.3, 17.6; 32: 74.4, 22.1.
+// each workgroup leaves accumulators to be joined, 4: 128, 31.8; 8: 87, 21.2; 16: 73.3, 17.6; 32: 74.4, 22.1.  Lookup of 224 rows of
+// 5809 keys, two sequences, 8: 18.5; 1: 8.3.
 static void plan(AttendParams &p)
 {
     p.steps = (p.c.capacity + 63) / 64;

@@ -16,7 +16,6 @@ namespace intattn {
 
 namespace {
 
-constexpr int EHOLD = 24576; // slots whose keys registers hold
 constexpr int BINS = 2048, FEW = 256;
 
 constexpr uint64_t HELD = 1ull << 63;
@@ -47,10 +46,11 @@ template <int EWAVES> __device__ __forceinline__ int sum_of_waves(int mine, int 
     return all;
 }
 
-// ENT threads; HOLD: keys in registers
-template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_select_kernel(const EvictParams p)
+// ENT threads; MOST: rounds of them whose keys registers hold, 0: none
+template <int ENT, int MOST> __global__ __launch_bounds__(ENT) void evict_select_kernel(const EvictParams p)
 {
     constexpr int EWAVES = ENT / 64, PER = BINS / ENT;
+    constexpr bool HOLD = MOST > 0;
     __shared__ int bins[BINS], sums[3][EWAVES], chosen[3], n_few;
     __shared__ uint32_t least_weight[EWAVES], most_weight[EWAVES]; // of the keys of a wave that are not held
     __shared__ int free_keys[EWAVES];                              // and how many they are
@@ -77,7 +77,7 @@ template <int ENT, bool HOLD> __global__ __launch_bounds__(ENT) void evict_selec
     };
     // The keys (behind the last: above any), and planes of their own take what lies below keep as it is; gaps are filled by the
     // next launch.
-    constexpr int MOST = ENT == 1024 ? EHOLD / 1024 : 8, AT_ONCE = 8; // rounds where keys are held; loads of a thread in flight
+    constexpr int AT_ONCE = 8; // loads of a thread in flight
     constexpr int BATCHES = HOLD ? MOST / AT_ONCE : 1; // that are told apart, because registers have no index
     uint64_t key[HOLD ? MOST : 1];
     const int under = min(len, p.keep);
@@ -365,10 +365,14 @@ int launch_evict(const EvictParams &p_, void *room, void *stream)
     p.count = (int32_t *)room;
     p.moves = p.count + (int64_t)p.c.B * p.c.Hkv + p.c.B;
     const int groups = p.c.B * p.c.Hkv;
-    // a workgroup of 512 threads up to 4096 slots: its barriers are cheaper
-    const bool few = p.c.capacity <= 4096, hold = p.c.capacity <= EHOLD;
-    const int threads = few ? 512 : 1024;
-    void (*select)(const EvictParams) = few ? evict_select_kernel<512, true> : hold ? evict_select_kernel<1024, true> : evict_select_kernel<1024, false>;
+    // 512 threads where few slots leave more of them idle, and where a compute unit gets more than one workgroup, which it then holds at once
+    // (1024 threads and 512, us: 32 workgroups of 1150 keys 11.2, 9.8, of 4000 11.0, 10.7, 8 of 8000 16.7, 17.5; 480 of 1100 21.1, 13.7, of
+    // 4000 27.7, 18.8, of 6000 29.2, 22.0, of 8000 28.5, 24.0)
+    const bool half = p.c.capacity <= (groups > 256 ? 24 * 512 : 8 * 512);
+    void (*select)(const EvictParams) = evict_select_kernel<1024, 0>;
+    if (half) select = p.c.capacity <= 8 * 512 ? evict_select_kernel<512, 8> : evict_select_kernel<512, 24>;
+    else if (p.c.capacity <= 24 * 1024) select = evict_select_kernel<1024, 24>;
+    const int threads = half ? 512 : 1024;
     hipLaunchKernelGGL(select, dim3((uint32_t)groups), dim3((uint32_t)threads), 0, (hipStream_t)stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;

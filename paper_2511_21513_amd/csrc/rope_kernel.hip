@@ -92,7 +92,8 @@ int launch_rope(const RopeParams &p_, int dtype, void *stream)
     p.by_pairs = fast_div((uint32_t)(p.r.rot / 2));
     p.by_L = fast_div((uint32_t)p.L);
     // tokens of a workgroup where there are enough (8192 tokens of 40 heads, d 128, us: fp32, one 59.4, four 68.2; bf16, one 34.0, two 32.2,
-    // four 33.0; 128 000 tokens of 2 heads, fp32, d 64, two 97.9, 20 38.6); the heads of a token over several workgroups where there are few
+    // four 33.0; 128 000 tokens of 2 heads, fp32, d 64, two 97.9, 20 38.6); the heads of a
+    // token over several workgroups where there are few (8 tokens 3.5 us, in one workgroup each 4.0; 64 tokens 3.7, 4.2)
     p.tokens = tokens_of(all, p.per_token, 2, p.r.rot, TOKENS);
     const int64_t blocks = (all + p.tokens - 1) / p.tokens, rounds = ((int64_t)p.tokens * p.per_token + RNT - 1) / RNT;
     const int64_t parts = blocks >= 512 ? 1 : std::min<int64_t>(rounds, std::max<int64_t>(1, 512 / blocks));

@@ -494,11 +494,15 @@ EVICTS = [
     (1, 2, 64, 16, [900], 450, 0, 0, "wide"),               # weights of all exponents
     (2, 1, 64, 16, [1300, 700], 600, 0, 0, "narrow"),       # of three values next to each other, order by order
     (1, 2, 64, 16, [18000], 700, 3, 900, "held"),
+    (1, 1, 64, 16, [26000], 9000, 4, 500, "plain"),         # more keys than registers hold
+    (2, 1, 64, 16, [25000, 4000], 24000, 4, 64, "zeros"),
+    (270, 1, 64, 16, [5000, 4999, 4097] + [20] * 267, 4096, 2, 64, "equal"),  # workgroups of half the size
+    (300, 1, 64, 64, [12000, 11000, 90] + [1] * 297, 80, 2, 20, "plain"),
 ]
 
 
 @pytest.mark.parametrize("place", ["in place", "elsewhere"])
-@pytest.mark.parametrize("case", EVICTS, ids=str)
+@pytest.mark.parametrize("case", EVICTS, ids=lambda c: str(c)[:60])
 def test_evict(torch, ia, case, place):
     B, Hkv, d, page, lens, keep, sink, recent, how = case
     c = Case(torch, len(str(case)), B, Hkv, d, page, lens)
