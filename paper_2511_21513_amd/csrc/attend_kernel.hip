@@ -299,11 +299,13 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
     // (320 of up to 47 steps 44.1, 47.6; 512 of up to 62, d 64, 73.8, 78.1; 272 of up to 60 50.8, 55.0)
     const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
     const bool pipe = most_steps(p) > (groups > 256 ? 64 : 32);
-    // One wave where there is one step and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one; 8 of 30 keys 7.4, 8.0).
+    // One wave where there are few steps and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one, 8 of 30 keys 7.4, 8.0;
+    // 2000 of up to 120 20.2, 17.0, of up to 250 24.9, 22.2, 800 of them 15.1, 17.6).  Four for up to four steps (8 of 250 keys 8.0, with
+    // eight 8.3; 800 of 100 .. 250 15.1, 19.2; of five steps, 8 of 500 keys, 10.0, 9.2).
     // Four where two steps are in flight, a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their
     // way while the other looks up indices (1024 of 300 .. 6000 keys, one row, d 64, eight waves 125 us, four 116).
     const bool two = pipe && groups >= 320 && held_bytes(p) <= 60 * 1024;
-    const int waves = most_steps(p) <= 1 && groups > 512 ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
+    const int waves = most_steps(p) <= (groups >= 1536 ? 4 : groups > 512 ? 1 : 0) ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
     void (*kernel)(const AttendParams);
     if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
     else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;

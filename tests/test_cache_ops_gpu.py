@@ -668,6 +668,13 @@ def test_captured_step_replays_with_new_lengths(torch):
     ia.close()
 
 
+@pytest.mark.parametrize("d, page, most", [(64, 16, 250), (128, 8, 200), (128, 32, 60)])
+def test_forward_of_very_many_short_sequences(torch, ia, d, page, most):
+    c = Case(torch, d + most, 800, 2, d, page, [i % (most + 1) for i in range(799)] + [most], room=0)
+    got, wt, want, w = run_forward(torch, ia, c, 6, 1, None)
+    check_forward(torch, c, got, wt, want, w, 3, "int8")
+
+
 @pytest.mark.parametrize("weight", [False, True])
 def test_forward_of_as_many_rows_as_a_call_may_have(torch, ia, weight):
     c = Case(torch, 131, 2, 1, 64, 16, [700, 64], room=0)
