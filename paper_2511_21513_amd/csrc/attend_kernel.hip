@@ -305,10 +305,14 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
     // Four where two steps are in flight, a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their
     // way while the other looks up indices (1024 of 300 .. 6000 keys, one row, d 64, eight waves 125 us, four 116).
     const bool two = pipe && groups >= 320 && held_bytes(p) <= 60 * 1024;
-    const int waves = most_steps(p) <= (groups >= 1536 ? 4 : groups > 512 ? 1 : 0) ? 1 : most_steps(p) <= 4 || two ? 4 : 8;
+    // Sixteen for the only workgroup of a compute unit with one step in flight and sixteen steps or more (eight and sixteen, us: 64 of 1024
+    // keys 14.3, 13.1; 256 of up to 2000 25.1, 23.7; 8 of 700 11.0, 11.8).  Up to 32 steps' scores and their 30 KB fit LDS.
+    const bool most = !pipe && groups <= 256 && most_steps(p) >= 16;
+    const int waves = most_steps(p) <= (groups >= 1536 ? 4 : groups > 512 ? 1 : 0) ? 1 : most_steps(p) <= 4 || two ? 4 : most ? 16 : 8;
     void (*kernel)(const AttendParams);
     if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
     else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;
+    else if (waves == 16) kernel = attend_kernel<D, 16, WHOLE, false>;
     else kernel = pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
                        (hipStream_t)stream, p);

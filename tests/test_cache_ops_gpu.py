@@ -282,7 +282,8 @@ def test_forward_of_long_sequences(torch, ia, rows, d, page, n):
 
 
 @pytest.mark.parametrize("rows, d, page, lens", [(16, 64, 16, [2900, 0, 2112, 2113, 64]), (13, 128, 24, [2600, 2560, 1]), (9, 64, 64, [4800, 3840, 3000]), (4, 64, 16, [2300, 2048, 70, 0]),
-                                                  (4, 128, 16, [1500, 900]), (4, 64, 8, [2200, 65]), (2, 64, 64, [4200, 4096, 65])])
+                                                  (4, 128, 16, [1500, 900]), (4, 64, 8, [2200, 65]), (2, 64, 64, [4200, 4096, 65]), (16, 128, 64, [2048, 2000, 1]),
+                                                  (5, 128, 8, [1030, 64, 0])])
 def test_forward_of_long_sequences_among_many_short_ones(torch, ia, rows, d, page, lens):
     """Enough sequences for a workgroup each (176), or more than one to a compute unit (340), and a few of them with more scores than it
     holds."""
