@@ -3,7 +3,7 @@
 // IndexSoftmax needs the exact row maximum before any index and the exact row sum before any probability, so a row's keys are met
 // three times; K and V are read once each, because the scores, and then their table indices, stay in LDS.  Steps whose scores do not
 // fit have room for their indices there, and K of these is read again for them: with 32 sequences of 4000 to 12400 keys, 8 KV heads of
-// four rows and d 128, 135 us, 4.2 TB/s of the bytes that have to move (the three launches of attend_split.hip 144).  A workgroup
+// four rows and d 128, 137 us, 4.1 TB/s of the bytes that have to move (the three launches of attend_split.hip 144).  A workgroup
 // takes all keys of a (sequence, KV head) and up to 16 rows of its query heads and tokens (what several blocks of rows draw from the
 // keys is added up by a second launch); its waves take every NW-th step of 64 keys and meet at the maxima and at the sums.
 #include "attend_common.h"
@@ -14,9 +14,8 @@ namespace intattn {
 
 namespace {
 
-template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p)
+template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p)
 {
-    constexpr int BUF = PIPE ? 2 : 1;
     using Place = typename Keys<D, WHOLE>::Place;
     using PlaceK = typename Keys<D, WHOLE>::PlaceK;
     constexpr int KB = D / 64, CT = D / 16, ACC_ROW = D + 1; // (rows of accumulators a bank apart)
@@ -36,12 +35,8 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     const int row = blk * 16 + n, head = kvh * p.group + row / p.L, t = row % p.L;
     RowScales scales;
     if (threadIdx.x < 16 && row < p.rows) scales = row_scales(p, b, head, t, kvh);
-    Place pv[2];
-    PlaceK pk[2];
-    if constexpr (!PIPE) {
-        pk[0] = keys.find_k(wave, lane);
-        pv[0] = keys.find_v(wave, lane);
-    }
+    const PlaceK first_k = keys.find_k(wave, lane);
+    const Place first_v = keys.find_v(wave, lane);
     const int len = cache_len(p.c, b), fresh = new_tokens(p.n_new, b, p.L, len), steps = (len + 63) / 64;
     const int held_rows = min(p.rows, 16);
     // weights: the only block of rows writes them, of several each what its rows draw to a plane of its own
@@ -62,30 +57,19 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     }
     if (threadIdx.x < 64) entry[threadIdx.x] = (uint8_t)(p.lut[threadIdx.x >> 2] >> (8 * (threadIdx.x & 3)));
 
-    // K of the wave's first step, and V where few steps follow, are on their way while the rows' parameters are formed (V otherwise
-    // while the row's sum is found).  PIPE: two steps in flight; requests past the last step repeat it, because with a branch around
-    // them a wait could no longer count them
-    v4i a[BUF][4][KB], qf[KB];
-    bool there[BUF][4];
-    uint32_t v[BUF][16][KB];
-    float old[BUF];
-    auto ask_v = [&](int s, const Place &from, uint32_t (&vv)[16][KB], float &w) {
-        keys.load_v(from, lane, vv);
-        w = 0.0f;
-        if (weight) w = weight[min(s * 64 + lane, len - 1)]; // uniform
+    // K and V of the wave's first step are on their way while the rows' parameters are formed.  (Further steps are asked for one at a time;
+    // the number of waves keeps keys on their way.  Places of a step asked for ahead of it: 102 and 100 us for 256 workgroups of 8192 keys,
+    // 116 and 117 for 1024 of up to 6000, and registers spilled for pages that are not whole runs.)
+    v4i a[4][KB], qf[KB];
+    bool there[4];
+    uint32_t v[16][KB];
+    float old;
+    auto ask_v = [&](int s, const Place &from) {
+        keys.load_v(from, lane, v);
+        old = weight ? weight[min(s * 64 + lane, len - 1)] : 0.0f; // uniform
     };
-    const int last = steps - 1;
-    if constexpr (PIPE) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + i * NW, last), lane);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) keys.load_k(pk[i], lane, a[i], there[i]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) pk[i] = keys.find_k(min(wave + (2 + i) * NW, last), lane);
-    } else {
-        keys.load_k(pk[0], lane, a[0], there[0]);
-        ask_v(wave, pv[0], v[0], old[0]);
-    }
+    keys.load_k(first_k, lane, a, there);
+    ask_v(wave, first_v);
     load_q<D>(p, b, kvh, row, kb, qf);
     if (threadIdx.x < 16) {
         RowParams rp = {1.0, 0.0f, 1, 0, 0, 31};
@@ -101,9 +85,9 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
 
     // Q.K^T and row maxima
     int top = HIDDEN;
-    auto take_k = [&](int s, const v4i (&ka)[4][KB], const bool (&kt)[4]) {
+    for (int s = wave; s < steps;) {
         v4i sc[4];
-        step_scores<D>(ka, kt, qf, limit - (s * 64 + 16 * kb), kb, sc);
+        step_scores<D>(a, there, qf, limit - (s * 64 + 16 * kb), kb, sc);
 #pragma unroll
         for (int ii = 0; ii < 4; ++ii) top = max(top, max(max(sc[ii][0], sc[ii][1]), max(sc[ii][2], sc[ii][3])));
         if (mine && s < held_to) {
@@ -111,28 +95,8 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) at[ii] = make_int4(sc[ii][0], sc[ii][1], sc[ii][2], sc[ii][3]);
         }
-    };
-    if constexpr (PIPE) {
-        for (int s = wave; s < steps; s += 2 * NW) {
-            take_k(s, a[0], there[0]);
-            keys.load_k(pk[0], lane, a[0], there[0]);
-            pk[0] = keys.find_k(min(s + 4 * NW, last), lane);
-            if (s + NW < steps) take_k(s + NW, a[1], there[1]);
-            keys.load_k(pk[1], lane, a[1], there[1]);
-            pk[1] = keys.find_k(min(s + 5 * NW, last), lane);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + i * NW, last), lane);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) ask_v(min(wave + i * NW, last), pv[i], v[i], old[i]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) pv[i] = keys.find_v(min(wave + (2 + i) * NW, last), lane);
-    } else {
-        for (int s = wave; s < steps;) {
-            take_k(s, a[0], there[0]);
-            s += NW;
-            if (s < steps) keys.load_k(keys.find_k(s, lane), lane, a[0], there[0]);
-        }
+        s += NW;
+        if (s < steps) keys.load_k(keys.find_k(s, lane), lane, a, there);
     }
     top = max(top, __shfl_xor(top, 16));
     top = max(top, __shfl_xor(top, 32));
@@ -166,9 +130,9 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
         PlaceK at = keys.find_k(held_to + wave, lane);
         for (int s = held_to + wave; s < steps; s += NW) {
             v4i sc[4];
-            keys.load_k(at, lane, a[0], there[0]);
+            keys.load_k(at, lane, a, there);
             at = keys.find_k(s + NW, lane);
-            step_scores<D>(a[0], there[0], qf, limit - (s * 64 + 16 * kb), kb, sc);
+            step_scores<D>(a, there, qf, limit - (s * 64 + 16 * kb), kb, sc);
             if (!mine) continue;
             uint32_t word[4];
 #pragma unroll
@@ -194,7 +158,7 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
     v4i acc[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = v4i{0, 0, 0, 0};
-    auto take_v = [&](int s, const uint32_t (&vv)[16][KB], float before) {
+    for (int s = wave; s < steps;) {
         uint32_t word[4] = {0, 0, 0, 0};
         if (mine) {
             const int4 x = *place(s);
@@ -207,29 +171,15 @@ template <int D, int NW, bool WHOLE, bool PIPE> __global__ __launch_bounds__(64 
             pf[j / 4] |= (int)(pr << (8 * (j & 3)));
         }
         if (!mine) pf = v4i{0, 0, 0, 0};
-        step_pv<D>(vv, pf, acc);
+        step_pv<D>(v, pf, acc);
         if (weight_out) { // uniform
             if (mine) widx[wave][n * 4 + kb] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
             const float drawn = drawn_by((const uint8_t *)widx[wave], share, held_rows, lane);
             const int slot = s * 64 + lane;
-            if (slot < len) weight_out[slot] = p.decay * before + drawn;
+            if (slot < len) weight_out[slot] = p.decay * old + drawn;
         }
-    };
-    if constexpr (PIPE) {
-        for (int s = wave; s < steps; s += 2 * NW) {
-            take_v(s, v[0], old[0]);
-            ask_v(min(s + 2 * NW, last), pv[0], v[0], old[0]);
-            pv[0] = keys.find_v(min(s + 4 * NW, last), lane);
-            if (s + NW < steps) take_v(s + NW, v[1], old[1]);
-            ask_v(min(s + 3 * NW, last), pv[1], v[1], old[1]);
-            pv[1] = keys.find_v(min(s + 5 * NW, last), lane);
-        }
-    } else {
-        for (int s = wave; s < steps;) {
-            take_v(s, v[0], old[0]);
-            s += NW;
-            if (s < steps) ask_v(s, keys.find_v(s, lane), v[0], old[0]);
-        }
+        s += NW;
+        if (s < steps) ask_v(s, keys.find_v(s, lane));
     }
     if (mine && wave < steps) {
 #pragma unroll
@@ -259,8 +209,9 @@ __global__ __launch_bounds__(256) void attend_weights_kernel(const AttendParams 
 
 } // namespace
 
-// LDS for the scores of a workgroup: all of them, or those of as many steps as leave room for the indices of the others
-static constexpr int HELD_BYTES = 136 * 1024;
+// LDS for the scores of a workgroup (beside 30 KB of sixteen waves): all of them, or those of as many steps as leave room for the indices
+// of the others
+static constexpr int HELD_BYTES = 130 * 1024;
 
 static int most_steps(const AttendParams &p) { return (p.c.capacity + 63) / 64; }
 static int step_rows(const AttendParams &p) { return 4 * (p.rows < 16 ? p.rows : 16); }
@@ -275,7 +226,7 @@ static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_
 // launch takes 8, a third or half for each step of the longest sequence in its workgroup (more where pages are not whole runs of 16
 // keys) and a little for its rows, or what all bytes take through the chip.  Three take 17 and what all bytes need.  Both have further
 // launches for more than one block of rows.  (8 KV heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and
-// 15, 1 x 2048 19.3 and 18.3, 8 x 1024 14 and 21, 8 x 4096 41 and 29, 16 x 4096 42 and 49, 16 x 8192 78 and 84, 32 x 8192 103 and 141;
+// 15, 1 x 2048 19.3 and 18.3, 8 x 1024 13 and 21, 8 x 4096 36 and 29, 16 x 4096 37 and 49, 16 x 8192 76 and 84, 32 x 8192 102 and 141;
 // one KV head of 32 rows, d 64, 32 x 1 .. 4380 keys 30 and 28.)
 static bool split_serves(const AttendParams &p, int d, bool weight)
 {
@@ -294,26 +245,21 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
-    // two steps in flight in the only workgroup of a compute unit (8 groups, 16 steps 12.7 us without, 17.2 with; 256 of up to 61, d 64,
-    // 28.9, 24.9; 128 of 128 88.3, 78.1); where there are more, later, because then registers are left for two workgroups of eight waves
-    // (320 of up to 47 steps 44.1, 47.6; 512 of up to 62, d 64, 73.8, 78.1; 272 of up to 60 50.8, 55.0)
+    const int steps = most_steps(p);
     const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
-    const bool pipe = most_steps(p) > (groups > 256 ? 64 : 32);
     // One wave where there are few steps and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one, 8 of 30 keys 7.4, 8.0;
     // 2000 of up to 120 20.2, 17.0, of up to 250 24.9, 22.2, 800 of them 15.1, 17.6).  Four for up to four steps (8 of 250 keys 8.0, with
-    // eight 8.3; 800 of 100 .. 250 15.1, 19.2; of five steps, 8 of 500 keys, 10.0, 9.2).
-    // Four where two steps are in flight, a compute unit gets more than one workgroup and its LDS holds two, so that one has keys on their
-    // way while the other looks up indices (1024 of 300 .. 6000 keys, one row, d 64, eight waves 125 us, four 116).
-    const bool two = pipe && groups >= 320 && held_bytes(p) <= 60 * 1024;
-    // Sixteen for the only workgroup of a compute unit with one step in flight and sixteen steps or more (eight and sixteen, us: 64 of 1024
-    // keys 14.3, 13.1; 256 of up to 2000 25.1, 23.7; 8 of 700 11.0, 11.8).  Up to 32 steps' scores and their 30 KB fit LDS.
-    const bool most = !pipe && groups <= 256 && most_steps(p) >= 16;
-    const int waves = most_steps(p) <= (groups >= 1536 ? 4 : groups > 512 ? 1 : 0) ? 1 : most_steps(p) <= 4 || two ? 4 : most ? 16 : 8;
-    void (*kernel)(const AttendParams);
-    if (waves == 1) kernel = attend_kernel<D, 1, WHOLE, false>;
-    else if (waves == 4) kernel = pipe ? attend_kernel<D, 4, WHOLE, true> : attend_kernel<D, 4, WHOLE, false>;
-    else if (waves == 16) kernel = attend_kernel<D, 16, WHOLE, false>;
-    else kernel = pipe ? attend_kernel<D, 8, WHOLE, true> : attend_kernel<D, 8, WHOLE, false>;
+    // eight 8.3; 800 of 100 .. 250 15.1, 19.2; of five steps, 8 of 500 keys, 10.0, 9.2).  Sixteen from sixteen steps on for the only
+    // workgroup of a compute unit (eight and sixteen, us: 64 of 1024 keys 14.3, 13.1; 256 of up to 2000 25.1, 23.7; 8 of 700 11.0, 11.8);
+    // eight where there are more and LDS holds two of them, so that one has keys on their way while the other looks up indices (512 of up
+    // to 3700 keys 66.9, with sixteen 73.6).  Two steps of a wave on their way, for which registers are left with eight waves, took 42.4 us
+    // for 128 of 4096 keys, sixteen waves 36.7; 101.7 and 101.4 for 256 of 8192; 89.5 and 80.4 for 280 of 2044 .. 6132.
+    const bool two = groups > 256 && 2 * (held_bytes(p) + 22400) <= 160 * 1024;
+    const int waves = steps <= (groups >= 1536 ? 4 : groups > 512 ? 1 : 0) ? 1 : steps <= 4 ? 4 : steps >= 16 && !two ? 16 : 8;
+    void (*kernel)(const AttendParams) = waves == 1   ? attend_kernel<D, 1, WHOLE>
+                                         : waves == 4 ? attend_kernel<D, 4, WHOLE>
+                                         : waves == 8 ? attend_kernel<D, 8, WHOLE>
+                                                      : attend_kernel<D, 16, WHOLE>;
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
                        (hipStream_t)stream, p);
     if (drawn_room(p, p.weight) > 0)
