@@ -77,12 +77,15 @@ __device__ __forceinline__ void transpose4(const uint32_t w0, const uint32_t w1,
 // Where lanes find their keys.  WHOLE: pages of a multiple of 16 keys whose rows follow each other, so that 16 keys from a multiple of 16
 // on are one run of 16 d bytes: one look into the table, and offsets that are part of the instruction (with a stride that is not known
 // the sixteen addresses of a step of V took 32 registers).  Keys past the end are read where the table says, which does not wait for
-// the length, and keys of pages that are not there from the pool's first page (the probability of either is 0).  V that is read once
+// the length, and keys of pages that are not there from the pool's first page (the probability of either is 0); what lies past the last
+// slot that a sequence may have is read from its last key, or, where lanes read runs, from the start of its last run, which ends inside
+// its page because the page's size is a multiple of the run's.  V that is read once
 // is read in whole lines past the caches (8 KiB blocks in no order: 6.1 TB/s, 5.4 through them); half lines of K need the cache.
 //
 // find_*() asks the table, load_*() for the keys.  They are apart so that a loop can ask for the places of a step before it asks for the
 // keys of an earlier one: loads come back in order, and a place asked for last could only be waited for together with every key
 // that is on its way.  (Scalar loads, which are counted apart, miss their cache too often: 4.6 -> 6.4 us for the first launch on 700 keys.)
+// Every address that is formed for K and V comes from find_k(), find_v(), k_offset() and v_offset(), which the host can call as well.
 template <int D, bool WHOLE> struct Keys {
     const CacheParams &c;
     const int32_t *row;
@@ -94,33 +97,46 @@ template <int D, bool WHOLE> struct Keys {
     struct PlaceK {
         Place p[WHOLE ? 1 : 4];
     };
-    __device__ __forceinline__ Place find(int slot) const
+    // of a slot that is a multiple of RUN, a power of two: the first of as many keys that the lane reads from there
+    template <int RUN> __host__ __device__ __forceinline__ Place find(int slot) const
     {
-        slot = min(slot, c.capacity - 1);
+        const int last = (c.capacity - 1) & -RUN;
+        slot = slot < last ? slot : last;
         const int n = quotient(slot, c.by_page);
         return Place{row[n], slot - n * c.page_size};
     }
-    __device__ __forceinline__ bool there(const Place &p) const { return (uint32_t)p.entry < (uint32_t)c.n_pages; }
+    __host__ __device__ __forceinline__ bool there(const Place &p) const { return (uint32_t)p.entry < (uint32_t)c.n_pages; }
     // the lane's four keys 4 m + i of the step
-    __device__ __forceinline__ PlaceK find_k(int step, int lane) const
+    __host__ __device__ __forceinline__ PlaceK find_k(int step, int lane) const
     {
         PlaceK k;
 #pragma unroll
-        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) k.p[i] = find(step * 64 + 4 * (lane & 15) + i);
+        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) k.p[i] = find<WHOLE ? 4 : 1>(step * 64 + 4 * (lane & 15) + i);
         return k;
     }
     // the lane's sixteen keys from 16 kb on; not WHOLE: key 16 kb + m of them
-    __device__ __forceinline__ Place find_v(int step, int lane) const { return find(step * 64 + 16 * (lane >> 4) + (WHOLE ? 0 : lane & 15)); }
+    __host__ __device__ __forceinline__ Place find_v(int step, int lane) const { return find<WHOLE ? 16 : 1>(step * 64 + 16 * (lane >> 4) + (WHOLE ? 0 : lane & 15)); }
+
+    // bytes from the pool's first to the first 16 (and, 64 further, the second) of key i of the lane's four
+    __host__ __device__ __forceinline__ int64_t k_offset(const PlaceK &k, int i, int lane) const
+    {
+        const Place &p = k.p[WHOLE ? 0 : i];
+        const bool is = there(p);
+        return head_k + (is ? p.entry : 0) * c.ks[0] + (is ? p.at : 0) * (WHOLE ? D : c.ks[2]) + 16 * (lane >> 4) + (WHOLE ? i * D : 0);
+    }
+    // and to the lane's channels of the key at this place of this page, which are there; WHOLE: of the first of a run of sixteen, D bytes apart
+    __host__ __device__ __forceinline__ int64_t v_offset(int page, int at, int lane) const
+    {
+        return head_v + page * c.vs[0] + at * (WHOLE ? D : c.vs[2]) + (lane & 15) * (D / 16);
+    }
 
     // 16 bytes of each of the lane's four keys, channels 16 kb + 64 j on; is[i]: the key's page is there
     __device__ __forceinline__ void load_k(const PlaceK &k, int lane, v4i (&a)[4][D / 64], bool (&is)[4]) const
     {
-        const int kb = lane >> 4;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const Place &p = k.p[WHOLE ? 0 : i];
-            is[i] = there(p);
-            const int8_t *from = c.k + head_k + (is[i] ? p.entry : 0) * c.ks[0] + (is[i] ? p.at : 0) * (WHOLE ? D : c.ks[2]) + 16 * kb + (WHOLE ? i * D : 0);
+            is[i] = there(k.p[WHOLE ? 0 : i]);
+            const int8_t *from = c.k + k_offset(k, i, lane);
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) a[i][j] = *(const v4i *)(from + 64 * j);
         }
@@ -130,11 +146,11 @@ template <int D, bool WHOLE> struct Keys {
     {
         const bool is = there(p);
         const int page = is ? p.entry : 0, at = is ? p.at : 0;
-        const int8_t *const from = c.v + head_v + (lane & 15) * (D / 16) + (WHOLE ? page * c.vs[0] + at * D : 0);
+        const int8_t *const from = c.v + (WHOLE ? v_offset(page, at, lane) : 0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int8_t *key = from + i * D;
-            if constexpr (!WHOLE) key = from + __shfl(page, (lane & 48) + i) * c.vs[0] + __shfl(at, (lane & 48) + i) * c.vs[2];
+            if constexpr (!WHOLE) key = from + v_offset(__shfl(page, (lane & 48) + i), __shfl(at, (lane & 48) + i), lane);
             if constexpr (D == 128) {
                 v2i w;
                 if constexpr (ONCE) w = __builtin_nontemporal_load((const v2i *)key);
