@@ -331,7 +331,8 @@ INTATTN_API int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cach
  * The attention pipeline (steps 1 to 8 at the top of this file) for the newest tokens of each sequence over the cache: query
  * token t of sequence b sees slots j <= lens[b] - n_new[b] + t, tokens from n_new[b] on are padding.  A row that sees no key
  * comes out as zeros.  scale_q has a value for each token and head.  The output is INT8 as from intattn_forward, or
- * P_hat . V_hat s_V / 255 in floating point.  With weight, each slot j < lens[b] of each KV head gets
+ * P_hat . V_hat s_V / 255 in floating point.  (A ratio s_V / (255 s_O) from 2^30 on, or below 2^-32, which no multiplier stands for,
+ * takes every accumulator but 0 to +-127, or all of them to 0.)  With weight, each slot j < lens[b] of each KV head gets
  *   weight_out = decay * weight + sum over the rows of its query heads and tokens of E_hat / rowSum(E_hat)
  * in fp32 (slots behind stay as they are).  out must not alias the inputs.
  */

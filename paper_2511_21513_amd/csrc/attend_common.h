@@ -31,7 +31,7 @@ __device__ __forceinline__ RowScales row_scales(const AttendParams &p, int b, in
 __device__ __forceinline__ bool row_params(const AttendParams &p, const RowScales &s, RowParams &rp)
 {
     const float sq = s.q, sk = s.k, sv = s.v, so = s.out;
-    bool ok = good_cache_scale(sq) && good_cache_scale(sk) && good_cache_scale(sv) && good_cache_scale(so);
+    const bool ok = good_cache_scale(sq) && good_cache_scale(sk) && good_cache_scale(sv) && good_cache_scale(so);
     double c = 1.0;
     if (ok) {
         const double alpha = ((double)sq * (double)sk) / p.sqrt_d;
@@ -54,8 +54,11 @@ __device__ __forceinline__ bool row_params(const AttendParams &p, const RowScale
             e += 1;
         }
         const int sh = 31 - e;
-        if (!(r > 0.0) || sh < 1 || sh > 62) ok = false;
-        else {
+        // past a multiplier's range the formula is simple: accumulators, below 2^17, stay below a half, or saturate from 1 on
+        if (sh < 1) {
+            rp.mult = 1 << 30;
+            rp.shift = 1;
+        } else if (sh <= 62) {
             rp.mult = (int32_t)M;
             rp.shift = sh;
         }
