@@ -323,6 +323,49 @@ def _rotation(torch, B, L, device, pos, freq, axis, pairing, inverse):
     return (2 * n, int(pairing == "halves"), axes, int(bool(inverse)), pos.data_ptr(), *pos.stride(), freq.data_ptr(), axis or b"")
 
 
+def _whole_rows(torch, g):
+    """A gradient that autograd hands on, which may have any strides, as a tensor that the kernels can read."""
+    s0, s1, s2, s3 = g.stride()
+    if s3 == 1 and not (g.data_ptr() | (s0 | s1 | s2) * g.element_size()) & 15:
+        return g
+    return g.clone(memory_format=torch.contiguous_format)
+
+
+_rope_function = None
+
+
+def _differentiable_rope(torch):
+    """The autograd function of ``IntAttn.rope``: its gradient is the rotation backwards, a rope itself."""
+    global _rope_function
+    if _rope_function is None:
+
+        class Rope(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, ia, pos, freq, axis, pairing, inverse, stream, *xs):
+                axis = None if axis is None else bytes(axis)  # (the caller may change the list)
+                ctx.how = (ia, axis, pairing, inverse)
+                ctx.save_for_backward(pos, freq)  # (changed in place before the backward pass, torch raises)
+                ctx.set_materialize_grads(False)
+                outs = tuple(ia.rope(xs, pos, freq, axis=axis, pairing=pairing, inverse=inverse, stream=stream))
+                ctx.mark_non_differentiable(*(o for o, needed in zip(outs, ctx.needs_input_grad[7:]) if not needed))
+                return outs
+
+            @staticmethod
+            def backward(ctx, *gs):
+                ia, axis, pairing, inverse = ctx.how
+                pos, freq = ctx.saved_tensors
+                those = [i for i, g in enumerate(gs) if g is not None and ctx.needs_input_grad[7 + i]]
+                grads = [None] * len(gs)
+                if those:
+                    got = ia.rope([_whole_rows(torch, gs[i]) for i in those], pos, freq, axis=axis, pairing=pairing, inverse=not inverse)
+                    for i, g in zip(those, got):
+                        grads[i] = g
+                return (None,) * 7 + tuple(grads)
+
+        _rope_function = Rope
+    return _rope_function
+
+
 class PagedCache:
     """A paged INT8 key/value cache (``intattn_cache``): the caller's tensors, checked once, and the struct that points at them.
 
@@ -620,7 +663,8 @@ class IntAttn:
     def rope(self, x, pos, freq, *, axis=None, pairing="adjacent", inverse=False, out=None, stream=None):
         """intattn_rope on a [B, H, L, d] tensor, or on two with the same B, L, d (Q and K): new tensors, or ``out``, which may be
         ``x``.  ``pos``: int32 [axes, B, L] (or [B, L]); ``freq``: float64 [rot / 2], radians per position of each pair, on the
-        device; ``axis``: a list of each pair's axis (None: all the first).  ``inverse``: the gradient's rotation."""
+        device; ``axis``: a list of each pair's axis (None: all the first).  ``inverse``: the gradient's rotation, which autograd
+        takes by itself where x requires a gradient (then there is no ``out``, and ``freq`` has no gradient of its own)."""
         import torch
 
         one = torch.is_tensor(x)
@@ -629,6 +673,14 @@ class IntAttn:
         if not 1 <= n <= 2:
             raise ValueError("one tensor or two, and as many outputs")
         a, b = xs[0], xs[-1]
+        if torch.is_grad_enabled():
+            if freq.requires_grad:
+                raise ValueError("freq has no gradient: detach it")
+            if out is not None and (a.requires_grad or b.requires_grad or any(t.requires_grad for t in ([out] if torch.is_tensor(out) else out))):
+                raise ValueError("out does not go with tensors that require a gradient")
+            if a.requires_grad or b.requires_grad:
+                outs = _differentiable_rope(torch).apply(self, pos, freq, axis, pairing, inverse, stream, *xs)
+                return outs[0] if one else list(outs)
         B, H, L, d = shape = a.shape
         dtype, dev, es = a.dtype, a.get_device(), a.element_size()
         code = _float_types().get(dtype)
@@ -640,7 +692,8 @@ class IntAttn:
             t0, t1, t2, _ = _rows(b, "x", dtype, (B, H2, L, d), dev)
         else:
             H2, t0, t1, t2 = 0, s0, s1, s2
-        if out is None:
+        given = out is not None
+        if not given:
             o, o0, o1, o2 = p, p0, p1, p2 = _like(torch, a, dtype)
             if n == 2:
                 p, p0, p1, p2 = _like(torch, b, dtype)
@@ -657,6 +710,8 @@ class IntAttn:
                           s0 * es, s1 * es, s2 * es, t0 * es, t1 * es, t2 * es, o0 * es, o1 * es, o2 * es, p0 * es, p1 * es, p2 * es,
                           *_rotation(torch, B, L, dev, pos, freq, axis, pairing, inverse))
         self._done(self._lib.intattn_rope(self._ctx, args, self._stream(dev, stream)))
+        if given:
+            torch.autograd.graph.increment_version(outs)  # (a graph that has kept one of them raises in its backward pass)
         return out
 
     def cache_append(self, cache: PagedCache, k, v, q=None, *, n_new=None, pos=None, freq=None, axis=None, pairing="adjacent",
