@@ -783,6 +783,8 @@ class IntAttn:
             weight_out = weight if weight_out is None else weight_out
             w = _slots(weight, "weight", torch.float32, B, cache.Hkv, slots, dev)
             planes = (weight.data_ptr(), weight_out.data_ptr(), *w, *(w if weight_out is weight else _slots(weight_out, "weight_out", torch.float32, B, cache.Hkv, slots, dev)))
+        elif weight_out is not None:
+            raise ValueError("weight_out needs weight")
         args = _CACHE_FORWARD.pack(Hq, L, int(max_len), code, q.data_ptr(), q0, q1, q2, scale_q.data_ptr(), _ptr(n_new), out.data_ptr(),
                                    o0 * es, o1 * es, o2 * es, _ptr(scale_out), *planes, float(decay), per_head)
         self._done(self._lib.intattn_cache_forward(self._ctx, cache._ref, args, self._stream(dev, stream)))
