@@ -356,7 +356,9 @@ typedef struct {
 
 /* Enqueues the attention on hip_stream.  Calls that need more room than the context has for the scores allocate it (a
  * captured call is refused instead: intattn_cache_reserve first); room is never moved or given back before
- * intattn_destroy.  Calls on one context must not overlap in time. */
+ * intattn_destroy.  Room for scores is 4 bytes for each row and key, by max_len (0: max_pages * page_size) and not by lens, of as
+ * many KV heads of sequences as 1 GiB serves, of one at least: calls with more take them one part after the other, through the same room.
+ * Calls on one context must not overlap in time. */
 INTATTN_API int intattn_cache_forward(intattn_ctx *ctx, const intattn_cache *cache, const intattn_cache_forward_args *args,
                                       void *hip_stream);
 

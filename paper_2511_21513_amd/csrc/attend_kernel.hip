@@ -28,7 +28,7 @@ template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void 
     extern __shared__ int4 held[];
     __shared__ int4 widx[NW][64];               // indices of a wave's step
 
-    const int b = blockIdx.x / p.c.Hkv, kvh = blockIdx.x % p.c.Hkv, blk = blockIdx.y;
+    const int group = p.first + blockIdx.x, b = group / p.c.Hkv, kvh = group % p.c.Hkv, blk = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kb = lane >> 4;
     const Keys<D, WHOLE> keys{p.c, p.c.table + b * p.c.table_stride, kvh * p.c.ks[1], kvh * p.c.vs[1]};
     // (asked for before the length is known, and the scales before keys that a wait for them would have to wait for as well)
@@ -198,7 +198,7 @@ template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void 
 // Weights where a KV head has several blocks of rows: what they have drawn, block by block.
 __global__ __launch_bounds__(256) void attend_weights_kernel(const AttendParams p)
 {
-    const int b = blockIdx.y / p.c.Hkv, kvh = blockIdx.y % p.c.Hkv, slot = blockIdx.x * 256 + threadIdx.x;
+    const int group = p.first + blockIdx.y, b = group / p.c.Hkv, kvh = group % p.c.Hkv, slot = blockIdx.x * 256 + threadIdx.x;
     if (slot >= cache_len(p.c, b)) return;
     const float *const of = p.drawn + (int64_t)blockIdx.y * p.blocks * p.c.capacity + slot;
     float drawn = 0.0f;
@@ -239,15 +239,16 @@ static bool split_serves(const AttendParams &p, int d, bool weight)
     return three < one;
 }
 
-// room: what each block of rows draws, [group][block][capacity]
-static int64_t drawn_room(const AttendParams &p, bool weight) { return weight && p.blocks > 1 ? 4 * (int64_t)p.c.B * p.c.Hkv * p.blocks * p.c.capacity : 0; }
+// room: what each block of rows draws, [group][block][capacity]; of a launch that takes `groups` groups
+static int64_t drawn_room(const AttendParams &p, int64_t groups, bool weight) { return weight && p.blocks > 1 ? 4 * groups * p.blocks * p.c.capacity : 0; }
 
-template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, void *stream)
+// groups from p.first on
+template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, int64_t n, void *stream)
 {
     AttendParams p = p_;
     p.held_steps = held_steps(p);
     const int steps = most_steps(p);
-    const int64_t groups = (int64_t)p.c.B * p.c.Hkv * p.blocks;
+    const int64_t groups = n * p.blocks;
     // One wave where there are few steps and the workgroups are many (1856 of 43 keys 29.3 us with four, 13.0 with one, 8 of 30 keys 7.4, 8.0;
     // 2000 of up to 120 20.2, 17.0, of up to 250 24.9, 22.2, 800 of them 15.1, 17.6).  Four for up to four steps (8 of 250 keys 8.0, with
     // eight 8.3; 800 of 100 .. 250 15.1, 19.2; of five steps, 8 of 500 keys, 10.0, 9.2).  Sixteen from sixteen steps on for the only
@@ -261,13 +262,16 @@ template <int D, bool WHOLE> static void launch_waves(const AttendParams &p_, vo
                                          : waves == 4 ? attend_kernel<D, 4, WHOLE>
                                          : waves == 8 ? attend_kernel<D, 8, WHOLE>
                                                       : attend_kernel<D, 16, WHOLE>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)n, (uint32_t)p.blocks), dim3((uint32_t)(64 * waves)), (uint32_t)held_bytes(p),
                        (hipStream_t)stream, p);
-    if (drawn_room(p, p.weight) > 0)
-        hipLaunchKernelGGL(attend_weights_kernel, dim3((uint32_t)((p.c.capacity + 255) / 256), (uint32_t)(p.c.B * p.c.Hkv)), dim3(256), 0, (hipStream_t)stream, p);
+    if (p.weight && p.blocks > 1)
+        hipLaunchKernelGGL(attend_weights_kernel, dim3((uint32_t)((p.c.capacity + 255) / 256), (uint32_t)n), dim3(256), 0, (hipStream_t)stream, p);
 }
 
-static int64_t room_of(const AttendParams &p, int d, bool weight) { return split_serves(p, d, weight) ? attend_split_room(p, d, nullptr, nullptr) : drawn_room(p, weight); }
+static int64_t room_of(const AttendParams &p, int d, bool weight)
+{
+    return split_serves(p, d, weight) ? attend_split_room(p, d) : std::min(drawn_room(p, (int64_t)p.c.B * p.c.Hkv, weight), SCORE_ROOM);
+}
 
 int64_t attend_room(const AttendParams &p, int d) { return room_of(p, d, p.weight); }
 
@@ -288,9 +292,17 @@ int launch_attend(const AttendParams &p_, int d, void *room, void *stream)
     AttendParams p = p_;
     p.drawn = (float *)room;
     const bool whole = whole_pages(p.c, d);
-    if (d == 64) whole ? launch_waves<64, true>(p, stream) : launch_waves<64, false>(p, stream);
-    else whole ? launch_waves<128, true>(p, stream) : launch_waves<128, false>(p, stream);
-    return (int)hipGetLastError();
+    // the groups whose room that is: one needs less than SCORE_ROOM (256 blocks, and no more keys than LDS has indices for)
+    const int64_t all = (int64_t)p.c.B * p.c.Hkv, each = drawn_room(p, 1, p.weight), at_once = each > 0 ? std::min(all, SCORE_ROOM / each) : all;
+    for (int64_t first = 0; first < all; first += at_once) {
+        const int64_t n = std::min(at_once, all - first);
+        p.first = (int32_t)first;
+        if (d == 64) whole ? launch_waves<64, true>(p, n, stream) : launch_waves<64, false>(p, n, stream);
+        else whole ? launch_waves<128, true>(p, n, stream) : launch_waves<128, false>(p, n, stream);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    return (int)hipSuccess;
 }
 
 } // namespace intattn

@@ -24,11 +24,12 @@ constexpr int SBLK = 8, SROWS = 16 * SBLK; // rows of a workgroup in the first t
 struct Group {
     int b, kvh, len, fresh, steps;
 };
+// of place g in the room
 __device__ __forceinline__ Group group_of(const AttendParams &p, int g)
 {
     Group r;
-    r.b = g / p.c.Hkv;
-    r.kvh = g % p.c.Hkv;
+    r.b = (p.first + g) / p.c.Hkv;
+    r.kvh = (p.first + g) % p.c.Hkv;
     r.len = cache_len(p.c, r.b);
     r.fresh = new_tokens(p.n_new, r.b, p.L, r.len);
     r.steps = (r.len + 63) / 64;
@@ -383,10 +384,10 @@ __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p
 // 30011, d 128, us): scores, short workgroups, 4: 59.0, 9.1; 16: 69.5, 11.0.  Lookup, 8: 12.9, 4.6; 32: 10.2, 5.3.  Values, where
 // each workgroup leaves accumulators to be joined, 4: 128, 31.8; 8: 87, 21.2; 16: 73.3, 17.6; 32: 74.4, 22.1.  Lookup of 224 rows of
 // 5809 keys, two sequences, 8: 18.5; 1: 8.3.
-static void plan(AttendParams &p)
+static void plan(AttendParams &p, int64_t groups)
 {
     p.steps = (p.c.capacity + 63) / 64;
-    const int64_t all = (int64_t)p.steps * p.c.B * p.c.Hkv;
+    const int64_t all = p.steps * groups;
     // as many steps as leave `workgroups` workgroups, between `least` and what makes `most` chunks of a sequence
     auto steps_of = [&](int64_t workgroups, int64_t least, int64_t most) {
         const int64_t c = std::max(std::max((all + workgroups - 1) / workgroups, least), (p.steps + most - 1) / most);
@@ -401,11 +402,10 @@ static void plan(AttendParams &p)
     p.chunks = (p.steps + p.chunk_steps - 1) / p.chunk_steps;
 }
 
-int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParams *out)
+// bytes of room for `groups` groups, laid out from `room` on
+static int64_t lay_out(AttendParams &p, int d, int64_t groups, void *room)
 {
-    AttendParams p = p_;
-    plan(p);
-    const int64_t groups = (int64_t)p.c.B * p.c.Hkv;
+    plan(p, groups);
     int64_t at = 0;
     auto take = [&](int64_t words) {
         int32_t *const m = room ? (int32_t *)room + at : nullptr;
@@ -419,17 +419,24 @@ int64_t attend_split_room(const AttendParams &p_, int d, void *room, AttendParam
     p.arrived = take(groups * p.blocks);
     p.row_sum = take(groups * p.rows);
     p.row_params = (RowParams *)take(groups * p.rows * (int64_t)(sizeof(RowParams) / 4));
-    if (out) *out = p;
     return 4 * at;
+}
+
+// what all groups need; where that is more than SCORE_ROOM, that much, or what one group needs.  (No less for more rows: reservations.)
+int64_t attend_split_room(const AttendParams &p_, int d)
+{
+    AttendParams p = p_;
+    const int64_t all = lay_out(p, d, (int64_t)p.c.B * p.c.Hkv, nullptr);
+    return all <= SCORE_ROOM ? all : std::max(SCORE_ROOM, lay_out(p, d, 1, nullptr));
 }
 
 // Waves of a workgroup of the third launch: eight where they are no more than CUs, so that each has its keys on their way at once (four
 // rows, d 128, 8 KV heads, us with four waves and with eight: 1 x 30011 keys 18.3, 16.4; 1 x 100000 36.5, 31.5; 2 x 8000 13.8, 13.0; in
 // more workgroups, 4 x 4000 .. 12400, 19.0, 25.9).
-template <int D, bool WHOLE> static void launch_values(const AttendParams &p, hipStream_t st)
+template <int D, bool WHOLE> static void launch_values(const AttendParams &p, uint32_t groups, hipStream_t st)
 {
-    const dim3 grid((uint32_t)p.chunks, (uint32_t)(p.c.B * p.c.Hkv), (uint32_t)p.blocks);
-    const bool eight = (int64_t)p.chunks * p.c.B * p.c.Hkv * p.blocks <= 256;
+    const dim3 grid((uint32_t)p.chunks, groups, (uint32_t)p.blocks);
+    const bool eight = (int64_t)p.chunks * groups * p.blocks <= 256;
     void (*kernel)(const AttendParams);
     if (p.blocks > 1) kernel = eight ? cache_values_kernel<D, 8, WHOLE, false, false> : cache_values_kernel<D, 4, WHOLE, false, false>;
     else if (p.weight) kernel = eight ? cache_values_kernel<D, 8, WHOLE, true, true> : cache_values_kernel<D, 4, WHOLE, true, true>;
@@ -437,13 +444,13 @@ template <int D, bool WHOLE> static void launch_values(const AttendParams &p, hi
     hipLaunchKernelGGL(kernel, grid, dim3(eight ? 512 : 256), 0, st, p);
 }
 
-template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, hipStream_t st)
+template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, uint32_t groups, hipStream_t st)
 {
-    const uint32_t groups = (uint32_t)(p.c.B * p.c.Hkv), supers = (uint32_t)((p.rows + SROWS - 1) / SROWS);
+    const uint32_t supers = (uint32_t)((p.rows + SROWS - 1) / SROWS);
     if (p.blocks == 1) hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, true>), dim3((uint32_t)p.score_chunks, groups, 1), dim3(SNT), 0, st, p);
     else hipLaunchKernelGGL((cache_scores_kernel<D, WHOLE, false>), dim3((uint32_t)p.score_chunks, groups, supers), dim3(SNT), 0, st, p);
     hipLaunchKernelGGL(cache_lookup_kernel, dim3((uint32_t)p.lookup_chunks, groups, supers), dim3(SNT), 0, st, p);
-    launch_values<D, WHOLE>(p, st);
+    launch_values<D, WHOLE>(p, groups, st);
     if (p.blocks == 1) return;
     hipLaunchKernelGGL(cache_join_kernel<D>, dim3((uint32_t)((p.rows * D / 4 + JNT - 1) / JNT), groups), dim3(JNT), 0, st, p);
     if (p.weight) hipLaunchKernelGGL(cache_weights_kernel, dim3((uint32_t)((p.c.capacity + SNT - 1) / SNT), groups), dim3(SNT), 0, st, p);
@@ -451,13 +458,22 @@ template <int D, bool WHOLE> static void launch_split_d(const AttendParams &p, h
 
 int launch_attend_split(const AttendParams &p_, int d, void *room, void *stream)
 {
-    AttendParams p;
-    attend_split_room(p_, d, room, &p);
+    AttendParams p = p_;
     const bool whole = whole_pages(p.c, d);
     hipStream_t st = (hipStream_t)stream;
-    if (d == 64) whole ? launch_split_d<64, true>(p, st) : launch_split_d<64, false>(p, st);
-    else whole ? launch_split_d<128, true>(p, st) : launch_split_d<128, false>(p, st);
-    return (int)hipGetLastError();
+    const int64_t all = (int64_t)p.c.B * p.c.Hkv, bytes = attend_split_room(p, d);
+    int64_t at_once = all; // groups whose room that is
+    for (int64_t need; at_once > 1 && (need = lay_out(p, d, at_once, nullptr)) > bytes;) at_once = std::max<int64_t>(1, std::min(at_once - 1, at_once * bytes / need));
+    lay_out(p, d, at_once, room); // (one layout for all parts: fewer groups may be cut into more chunks, and need more)
+    for (int64_t first = 0; first < all; first += at_once) {
+        const int64_t n = std::min(at_once, all - first);
+        p.first = (int32_t)first;
+        if (d == 64) whole ? launch_split_d<64, true>(p, (uint32_t)n, st) : launch_split_d<64, false>(p, (uint32_t)n, st);
+        else whole ? launch_split_d<128, true>(p, (uint32_t)n, st) : launch_split_d<128, false>(p, (uint32_t)n, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    return (int)hipSuccess;
 }
 
 } // namespace intattn

@@ -115,8 +115,8 @@ int check_rotary(intattn_ctx *ctx, const intattn_rotary &r, int d, bool optional
     return INTATTN_OK;
 }
 
-// Room of at least `bytes` on the context.  A larger piece replaces a smaller one at least doubled, and the smaller stays
-// allocated: graphs that were captured with it may be replayed.
+// Room of at least `bytes` on the context.  A larger piece replaces a smaller one at least doubled, up to SCORE_ROOM, and the smaller
+// stays allocated: graphs that were captured with it may be replayed.
 int room(intattn_ctx *ctx, int64_t bytes, void *stream, bool may_launch, void **out)
 {
     *out = ctx->d_cache_room;
@@ -129,7 +129,7 @@ int room(intattn_ctx *ctx, int64_t bytes, void *stream, bool may_launch, void **
             return fail(ctx, INTATTN_ERR_NOMEM, "a captured call lacks room for its scores or moves: call intattn_cache_reserve before the capture");
     }
     ctx->cache_room_outgrown.reserve(ctx->cache_room_outgrown.size() + 1); // (throws before anything is allocated)
-    const size_t want = std::max((size_t)bytes, 2 * ctx->cache_room_bytes);
+    const size_t want = std::max((size_t)bytes, std::min(2 * ctx->cache_room_bytes, (size_t)SCORE_ROOM));
     void *m = nullptr;
     size_t got = want;
     hipError_t e = hipMalloc(&m, got);

@@ -6,6 +6,10 @@
 
 namespace intattn {
 
+// Bytes of room for scores that a call may ask for: with more (sequence, KV head) groups than that serves, the launches take some groups after
+// the others (one group may need more: 2.1 GiB with 4096 rows of 131 071 keys)
+constexpr int64_t SCORE_ROOM = 1ll << 30;
+
 struct CacheParams {
     int8_t *k, *v;
     int64_t ks[3], vs[3];      // bytes between pages, heads, keys
@@ -83,6 +87,7 @@ struct AttendParams {
     float decay;
     int32_t Hq, L, group;      // group = Hq / Hkv
     int32_t rows, blocks;      // group * L rows of a KV head, in blocks of 16
+    int32_t first;             // (sequence, KV head) whose part of the room is the first: that of the launch's first workgroups
     int32_t out_type;
     int32_t top;
     double clip, sqrt_d;
@@ -93,7 +98,7 @@ struct AttendParams {
     // keys split over workgroups (attend_split.hip): steps of a sequence of capacity slots, and for each launch the steps of a
     // workgroup and the workgroups of a sequence.  Room: scores [group][steps][4][rows][16], maxima and sums [group][chunks of that
     // launch][rows], accumulators [group][block of rows][chunks][16][d], arrivals [group][block of rows], sums and parameters
-    // [group][rows]; a group is a (sequence, KV head)
+    // [group][rows]; a group is a (sequence, KV head) from `first` on
     int32_t steps, score_steps, score_chunks, lookup_steps, lookup_chunks, chunk_steps, chunks;
     int32_t *scores, *part_max, *part_sum, *part_acc, *arrived, *row_sum;
     RowParams *row_params;
@@ -121,7 +126,7 @@ int64_t attend_room(const AttendParams &p, int d);
 // and for any with at most as many rows, with weights or without
 int64_t attend_room_upto(const AttendParams &p, int d);
 int launch_attend(const AttendParams &p, int d, void *room, void *stream);
-int64_t attend_split_room(const AttendParams &p, int d, void *room, AttendParams *out);
+int64_t attend_split_room(const AttendParams &p, int d);
 int launch_attend_split(const AttendParams &p, int d, void *room, void *stream);
 int64_t evict_room(const EvictParams &p);
 int launch_evict(const EvictParams &p, void *room, void *stream);
