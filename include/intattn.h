@@ -334,7 +334,7 @@ INTATTN_API int intattn_cache_append(intattn_ctx *ctx, const intattn_cache *cach
  * P_hat . V_hat s_V / 255 in floating point.  (A ratio s_V / (255 s_O) from 2^30 on, or below 2^-32, which no multiplier stands for,
  * takes every accumulator but 0 to +-127, or all of them to 0.)  With weight, each slot j < lens[b] of each KV head gets
  *   weight_out = decay * weight + sum over the rows of its query heads and tokens of E_hat / rowSum(E_hat)
- * in fp32 (slots behind stay as they are).  out must not alias the inputs.
+ * in fp32, added up in one order whatever else the call holds (slots behind stay as they are).  out must not alias the inputs.
  */
 typedef struct {
     int32_t Hq, L;             /* query heads, a multiple of Hkv; query tokens of a sequence; Hq / Hkv * L <= 4096 */

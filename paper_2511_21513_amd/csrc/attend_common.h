@@ -278,6 +278,10 @@ __device__ __forceinline__ float drawn_by(const uint8_t *idx, const float (*shar
     return sum;
 }
 
+// A key's weight after a call.  `drawn` is added up in one order whichever kernels a call takes, and so whatever else is in it: over the rows
+// of a block of 16, and then over the blocks.
+__device__ __forceinline__ float new_weight(const AttendParams &p, float old, float drawn) { return __builtin_fmaf(p.decay, old, drawn); }
+
 // N channels of an output row from ch (a multiple of N) on; mult and shift (INT8) or unit of the row's parameters
 template <int N> __device__ __forceinline__ void store_out(const AttendParams &p, float unit, int mult, int shift, uint8_t *at, int ch, const int (&acc)[N])
 {

@@ -176,7 +176,7 @@ template <int D, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW) void 
             if (mine) widx[wave][n * 4 + kb] = make_int4((int)word[0], (int)word[1], (int)word[2], (int)word[3]);
             const float drawn = drawn_by((const uint8_t *)widx[wave], share, held_rows, lane);
             const int slot = s * 64 + lane;
-            if (slot < len) weight_out[slot] = p.decay * old + drawn;
+            if (slot < len) weight_out[slot] = new_weight(p, old, drawn);
         }
         s += NW;
         if (s < steps) ask_v(s, keys.find_v(s, lane));
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void attend_weights_kernel(const AttendParams 
     float drawn = 0.0f;
 #pragma unroll 8
     for (int blk = 0; blk < p.blocks; ++blk) drawn += of[(int64_t)blk * p.c.capacity];
-    p.weight_out[b * p.wost[0] + kvh * p.wost[1] + slot] = p.decay * p.weight[b * p.wst[0] + kvh * p.wst[1] + slot] + drawn;
+    p.weight_out[b * p.wost[0] + kvh * p.wost[1] + slot] = new_weight(p, p.weight[b * p.wst[0] + kvh * p.wst[1] + slot], drawn);
 }
 
 } // namespace

@@ -251,7 +251,7 @@ template <int D, int NW, bool WHOLE, bool ONE, bool WEIGHT> __global__ __launch_
         if constexpr (WEIGHT) {
             if (mine) widx[wave][n * 4 + kb] = of.x;
             const float drawn = drawn_by((const uint8_t *)widx[wave], share, rows, lane);
-            if (s * 64 + lane < gr.len) weight_out[s * 64 + lane] = p.decay * of.old + drawn;
+            if (s * 64 + lane < gr.len) weight_out[s * 64 + lane] = new_weight(p, of.old, drawn);
         }
     };
     for (int s = first; s < s1; s += 2 * NW) {
@@ -371,11 +371,19 @@ __global__ __launch_bounds__(SNT) void cache_weights_kernel(const AttendParams p
         __syncthreads();
         if (mine) {
             const uint8_t *at = (const uint8_t *)(step_of(p, g, slot >> 6) + row0 * 4) + (slot & 63);
-#pragma unroll 16
-            for (int r = 0; r < rows; ++r) drawn += share[r][at[64 * r]];
+            for (int r0 = 0; r0 < rows; r0 += 16) { // a block of rows
+                float of_block = 0.0f;
+                if (rows - r0 >= 16) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) of_block += share[r0 + r][at[64 * (r0 + r)]];
+                } else {
+                    for (int r = r0; r < rows; ++r) of_block += share[r][at[64 * r]];
+                }
+                drawn += of_block;
+            }
         }
     }
-    if (mine) p.weight_out[gr.b * p.wost[0] + gr.kvh * p.wost[1] + slot] = p.decay * p.weight[gr.b * p.wst[0] + gr.kvh * p.wst[1] + slot] + drawn;
+    if (mine) p.weight_out[gr.b * p.wost[0] + gr.kvh * p.wost[1] + slot] = new_weight(p, p.weight[gr.b * p.wst[0] + gr.kvh * p.wst[1] + slot], drawn);
 }
 
 } // namespace
