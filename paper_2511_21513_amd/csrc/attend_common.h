@@ -215,9 +215,8 @@ template <int D> __device__ __forceinline__ void load_q(const AttendParams &p, i
     }
 }
 
-// (left of lanes without a row: any, as long as it does not hold the others up)
-// scores of the lane's row for its 16 keys, sc[ii][i] that of key 16 kb + 4 ii + i; HIDDEN past the row's limit (left: what is left
-// of it at the lane's first key) and where the page is not there
+// Scores of the lane's row for its 16 keys, sc[ii][i] that of key 16 kb + 4 ii + i; HIDDEN past the row's limit (left: what is left
+// of it at the lane's first key; lanes without a row give 16 or more, so that the others need not mask) and where the page is not there.
 template <int D> __device__ __forceinline__ void step_scores(const v4i (&a)[4][D / 64], const bool (&there)[4], const v4i (&qf)[D / 64], int left, int kb, v4i (&sc)[4])
 {
 #pragma unroll

@@ -5,8 +5,8 @@
 //   lookup   the row's maximum; scores become table indices (a byte each, in place), a sum for each row and chunk
 //   values   the row's sum; P.V of a chunk; the last workgroup of a KV head's chunks adds them up and writes the rows.  With more than
 //            one block of 16 rows a fourth launch does, and a fifth forms the weights.
-// K and V are read once, and the scores (4 bytes for each row and key against 2 d for a key) mostly stay in the caches between the
-// launches.  The chunks of all sequences are one grid of small workgroups, which evens out sequences of different lengths.
+// K is read once for each 128 rows of a KV head and V once for each 16, and the scores (4 bytes for each row and key against 2 d for a key)
+// mostly stay in the caches between the launches where rows are few.  The chunks of all sequences are one grid of small workgroups, which evens out sequences of different lengths.
 //
 // Scores of a step of 64 keys: [ii][row][kb] of four keys 16 kb + 4 ii each, so that a wave's stores are contiguous; the sixteen
 // indices of (row, kb) take the place of its first four scores.
