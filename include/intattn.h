@@ -31,9 +31,9 @@
  * intattn_index_softmax (Sec. 3.1-3.2 alone, on INT32 logits).  For serving from a paged INT8 cache: intattn_rope,
  * intattn_cache_append, intattn_cache_forward and intattn_cache_evict.
  *
- * The kernels for many query rows keep the L x L score matrix out of HBM; launches that split the keys of few
- * query rows, and of a paged cache, pass their scores through device memory of the context.  Results are a deterministic integer
- * function of the inputs (no dependence on tiling or launch shape).
+ * The kernels for many query rows keep the L x L score matrix out of HBM; launches that split the keys of
+ * few query rows, or of a paged cache, pass their scores through device memory of the context.  Results are a
+ * deterministic integer function of the inputs (no dependence on tiling or launch shape).
  *
  * All entry points return 0 on success or a negative INTATTN_ERR_* code; none throws or aborts.
  * A forward call enqueues its kernels and returns; it allocates device memory (hipMalloc / hipFree,
@@ -249,10 +249,11 @@ INTATTN_API int intattn_index_softmax(intattn_ctx *ctx, const intattn_softmax_ar
  * the pages of sequence b in order, so that its key number j (its slot) is key j % page_size of page table[b][j / page_size].
  * An entry that is not in 0 .. n_pages - 1 stands for a page that is not there: its keys are hidden, and nothing is written
  * to them.  lens[b], the number of slots in use, is taken as at least 0 and at most max_pages * page_size; the caller
- * keeps it, and widens the table before it passes that.  Sequences may share pages that none of them writes to.  Scales that are not finite and > 0 cannot be
- * reported by return code: rows that they belong to come out as zeros.  Outputs, pages that are written to and planes of
- * weights or orders must not lie over themselves or each other (a stride of 0 is refused where it shows).  Everything in the struct but the scalars is
- * DEVICE memory that the kernels read when they run: a captured call sees the lengths, tables and scales of its replay.
+ * keeps it, and widens the table before it passes that.  Sequences may share pages that none of them writes to.  Scales that
+ * are not finite and > 0 cannot be reported by return code: rows that they belong to come out as zeros.  Outputs, pages that are
+ * written to and planes of weights or orders must not lie over themselves or each other (a stride of 0 is refused where it shows).
+ * Everything in the struct but the scalars is DEVICE memory that the kernels read when they run: a captured call sees the lengths,
+ * tables and scales of its replay.
  */
 typedef struct {
     int32_t B, Hkv, d;         /* sequences, 1 .. 65535; KV heads, 1 .. 65535; head dimension, 64 or 128   */
@@ -302,8 +303,9 @@ INTATTN_API int intattn_rope(intattn_ctx *ctx, const intattn_rope_args *args, vo
 /*
  * New tokens: K rotated (rotary.rot = 0: not), K and V quantized with the cache's scales (Sec. 2.1, Eq. quant: the nearest
  * integer of the fp32 quotient x / s, ties to even, clamped to +-127) and written to slots lens[b] - n_new[b] + t, so the lengths
- * already count the new tokens (with a lens[b] past the table the last slots that there are: what they held is lost); Q, where Hq > 0, rotated and quantized with a scale for each token and head,
- * s = max|q| / 127 (max|q| floored at 1e-12), as intattn_cache_forward takes it.  Sequence b has n_new[b] tokens, the rest
+ * already count the new tokens (with a lens[b] past the table the last slots that there are: what they held is lost); Q, where
+ * Hq > 0, rotated and quantized with a scale for each token and head, s = max|q| / 127 (max|q| floored at 1e-12), as
+ * intattn_cache_forward takes it.  Sequence b has n_new[b] tokens, the rest
  * of its L are padding: nothing is written for their K and V, their integers and scales of Q are 0.  Inputs must be finite.
  */
 typedef struct {

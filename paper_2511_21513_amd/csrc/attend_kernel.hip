@@ -225,8 +225,8 @@ static int held_bytes(const AttendParams &p) { return 16 * step_rows(p) * (most_
 // Whether the keys are split over workgroups: where not even the indices fit LDS, or where a model of both times, in us, says so.  One
 // launch takes 8, a third or half for each step of the longest sequence in its workgroup (more where pages are not whole runs of 16
 // keys) and a little for its rows, or what all bytes take through the chip (one price for a step, whether LDS holds its scores or K is
-// read again).  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV heads of four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and
-// 15, 1 x 2048 18.0 and 17.3, 8 x 1024 13 and 21, 8 x 4096 35 and 30, 12 x 4096 36 and 35, 16 x 4096 37 and 48, 16 x 8192 75 and 83,
+// read again).  Three take 17 and what all bytes need.  Both have further launches for more than one block of rows.  (8 KV heads of
+// four rows, d 128, one launch against the sum of three: 1 x 700 keys 10.0 and 15, 1 x 2048 18.0 and 17.3, 8 x 1024 13 and 21, 8 x 4096 35 and 30, 12 x 4096 36 and 35, 16 x 4096 37 and 48, 16 x 8192 75 and 83,
 // 32 x 8192 102 and 141;
 // one KV head of 32 rows, d 64, 32 x 1 .. 4380 keys 30 and 28.)
 static bool split_serves(const AttendParams &p, int d, bool weight)
